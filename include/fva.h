@@ -8,6 +8,9 @@
  * pooled block similarities, Top-p with a Top-k floor, §2.1) and
  * block-sparse attention over the retained blocks (§2.1, §3.1), with the
  * Hilbert-curve block order of §3.1 as an alternative block organisation.
+ * Beside it stand the rotary positions of Q and K, and a paged 8-bit K/V
+ * cache with attention over it for video that is generated in pieces; no
+ * passage of the paper defines those.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -386,6 +389,180 @@ fva_status fva_attn_fp8v(const void* Q, const void* K, const uint8_t* V8, const 
 fva_status fva_attn_noalloc(const void* Q, const void* K, const void* V, const fva_qkv_desc* desc,
                             const fva_tiling* tiling, const int32_t* counts, const int32_t* kv_idx,
                             float softmax_scale, uint32_t flags, void* O, void* trace, void* stream);
+
+/*
+ * Rotary positions on three axes, for Q and K before fva_route / fva_attn
+ * (raster or curve order) and before fva_cache_store / fva_attn_cache
+ * (packed streams).
+ *
+ * The first R = dim_t + dim_y + dim_x channels of every row are turned in
+ * R / 2 pairs: the first dim_t / 2 pairs by the token's t, the next dim_y / 2
+ * by its y, the rest by its x; the other channels are copied. Pair i of an
+ * axis of d channels turns (u, v) by a = pos * theta^(-2 i / d):
+ *   u' = u cos a - v sin a,  v' = u sin a + v cos a,
+ * and by -a under inverse. The rotation is orthogonal, so inverse applied to
+ * the gradient of the outputs is the gradient of the inputs. Pair p is
+ * channels (2p, 2p + 1) under FVA_ROPE_PAIRS, (p, p + R / 2) under
+ * FVA_ROPE_HALVES (R then a multiple of 16).
+ *
+ * A token's position is that of its id in a stream of H x W frames in raster
+ * order: t = t0 + id / (H W), y = y0 + id / W % H, x = x0 + id % W. The id of
+ * token n of batch b is ids[b * ids_stride + n], or n where ids is NULL: NULL
+ * serves tokens in raster order, the perm of fva_curve_order curve order, the
+ * ids of fva_cache_plan packed streams. Rows of a negative id are copied.
+ * Angles are formed and reduced in fp64, the rotation is fp32, the result
+ * rounded once.
+ */
+#define FVA_BF16 0
+#define FVA_FP16 1
+#define FVA_FP32 2
+
+#define FVA_ROPE_PAIRS 0
+#define FVA_ROPE_HALVES 1
+
+typedef struct fva_rope_params {
+  int32_t H, W;                /* rows and columns of a frame */
+  int32_t dim_t, dim_y, dim_x; /* channels turned by each axis: even, >= 0, together <= 128 */
+  int32_t t0, y0, x0;          /* position of id 0 */
+  int32_t pairing;             /* FVA_ROPE_PAIRS or FVA_ROPE_HALVES */
+  int32_t inverse;             /* 0: by +a, 1: by -a */
+  double theta;                /* > 0 */
+} fva_rope_params;
+
+/*
+ * fva_rope -- Q_out = Q turned, and K_out = K turned unless K, K_out and
+ * k_desc are NULL. Q and K may differ in heads and strides, not in batch and
+ * tokens. Each output has its input's strides and may be its input (in
+ * place); any other overlap is the caller's error. dtype: the type of all
+ * four. ids: device int32, or NULL. No workspace.
+ * Errors: FVA_ERR_INVALID_ARG (NULL or misaligned pointers, dtype, pairing,
+ * theta), FVA_ERR_SHAPE (extents, odd or too many channels, rows that overlap
+ * or do not start on 16-byte boundaries), FVA_ERR_UNSUPPORTED (head_dim !=
+ * 128, batch or heads > 65535, R % 16 under FVA_ROPE_HALVES).
+ */
+fva_status fva_rope(const void* Q, void* Q_out, const fva_qkv_desc* q_desc, const void* K, void* K_out,
+                    const fva_qkv_desc* k_desc, int32_t dtype, const fva_rope_params* params, const int32_t* ids,
+                    int64_t ids_stride, void* stream);
+
+/*
+ * Paged K/V cache held in 8 bits, for video that is generated in pieces.
+ *
+ * A page holds `page` consecutive tokens of one stream for every K/V head:
+ * codes k8, v8 uint8 [pages, heads, page, 128] (OCP E4M3) and exponents
+ * k_exp, v_exp int32 [pages, heads], one power-of-two scale for each page and
+ * head: the value of a code is E4M3(code) * 2^e, with e = max(-100, min{e :
+ * amax * 2^-e <= 448}) over the page's tokens of that head. Token j of stream
+ * s lies in page block_table[s, j / page] at j % page; block_table is int32
+ * [streams, table_width]. All of it is the caller's memory.
+ *
+ * One step: fva_cache_plan gives the new tokens their pages, fva_rope turns Q
+ * and K by the plan's ids, fva_cache_store writes K and V to the plan's slots,
+ * fva_attn_cache attends. Nothing is read on the host, so that a step can be
+ * captured into a HIP graph and replayed on new lengths.
+ */
+typedef struct fva_cache {
+  int32_t pages, heads; /* pages of the pool, K/V heads */
+  int32_t page;         /* tokens of a page: 16, 32, 64 or 128 */
+  int32_t head_dim;     /* 128 */
+  uint8_t* k8;          /* 16-byte aligned */
+  uint8_t* v8;
+  int32_t* k_exp;
+  int32_t* v_exp;
+} fva_cache;
+
+/*
+ * fva_cache_plan -- block tables, slots and positions from request lengths,
+ * and the free pages.
+ *
+ * ring: int32 [ring_size], the free pages' ids in a ring; state: int32 [3],
+ * {head, count, unused}: ring[(head + i) % ring_size], i < count, are free.
+ * Stream s holds held[s] tokens and brings fresh[s] new ones; fresh[s] < 0
+ * ends it. In order of s, a growing stream takes the pages its new tokens
+ * need from the ring's front into its row of block_table, and an ended one
+ * gives its pages to the ring's back, from where the next call takes them. A
+ * stream is refused when its row is too narrow, or when the free pages do not
+ * suffice for its need together with that of the streams before it: it takes
+ * no page and its tokens get no slot.
+ *
+ * Outputs: block_table and ring (updated in place); kv_len int32 [streams] =
+ * held + fresh, held if refused, 0 if ended; q_start int32 [streams + 1], the
+ * streams' new tokens packed one behind the other (refused ones keep their
+ * rows); for row r of `tokens`: ids[r] the token's position in its stream and
+ * slots[r] = page id * page + position % page, both -1 for refused streams'
+ * rows and rows behind the last stream; state_out int32 [3] {head, count,
+ * refused streams}. kv_len must not be held or fresh, state_out not state.
+ * `tokens` is the rows of the buffers: tokens beyond it get no slot, but
+ * their pages. All pointers are device memory; no workspace.
+ * Errors: FVA_ERR_INVALID_ARG (NULL or misaligned pointers, outputs that are
+ * inputs), FVA_ERR_SHAPE (streams, ring_size or table_width <= 0, tokens <
+ * 0), FVA_ERR_UNSUPPORTED (page, streams > 2048, table_width * page >= 2^30).
+ */
+fva_status fva_cache_plan(const int32_t* held, const int32_t* fresh, int32_t streams, int32_t page,
+                          const int32_t* state, int32_t* ring, int32_t ring_size, int32_t* block_table,
+                          int32_t table_width, int32_t tokens, int32_t* kv_len, int32_t* q_start, int32_t* slots,
+                          int32_t* ids, int32_t* state_out, void* stream);
+
+/*
+ * fva_cache_store -- K and V (bf16, desc's layout, cache->heads heads) into
+ * the cache: row r = b * tokens + n goes to slot slots[r] (page * page size +
+ * offset; int32 [batch * tokens]); rows whose slot is negative or past the
+ * pool are left out.
+ *
+ * Rows with consecutive slots in one page form a run, which is appended to
+ * the page: a run that begins at offset 0 starts the page anew; one that
+ * begins later keeps the tokens before it, on the larger of the page's scale
+ * and the run's (their codes are rounded once more, to nearest even, when the
+ * scale grows), and leaves the bytes behind it as they are, which then stand
+ * on the page's new scale. The rows of one page must be one run in a call, as
+ * fva_cache_plan lays them out; a page that appears in two runs of one call
+ * (the same slot twice among them) ends with unspecified contents.
+ * Infinities are stored as the largest code, NaN as some finite value: the
+ * cache holds no NaN, and a masked key cannot reach any output.
+ * Errors: FVA_ERR_INVALID_ARG (NULL or misaligned pointers), FVA_ERR_SHAPE
+ * (heads differ, bad extents or strides), FVA_ERR_UNSUPPORTED (head_dim,
+ * page, 2^31 slots or more, batch * tokens * heads >= 2^30).
+ */
+fva_status fva_cache_store(const void* K, const void* V, const fva_qkv_desc* desc, const int32_t* slots,
+                           const fva_cache* cache, void* stream);
+
+/* Workspace bytes of fva_attn_cache: the partial results of tiles whose keys
+ * are split over workgroups, none (0) where the rows alone fill the device.
+ * Host only. */
+fva_status fva_attn_cache_workspace_size(const fva_qkv_desc* q_desc, const fva_cache* cache, int32_t table_width,
+                                         int32_t streams, int32_t max_q, size_t* bytes);
+
+/*
+ * fva_attn_cache -- attention of every stream's newest tokens over its cached
+ * tokens (the newest among them: store first).
+ *
+ * Q: bf16, desc's layout with batch 1: rows q_start[s] .. q_start[s + 1] - 1
+ * are the newest tokens of stream s, of which kv_len[s] are cached. Q has
+ * cache->heads * G heads; query head h reads K/V head h / G. Row i of a stream
+ * of q_len rows has position p = kv_len - q_len + i and sees the keys j with
+ *   max(0, end - window) <= j < min(end, kv_len),
+ *   end = kv_len if frame == 0, else (floor(p / frame) + 1) * frame
+ * (without the first bound if window == 0): frame 0 is attention to the whole
+ * cache, 1 is causal by token, H * W is causal by frame with the own frame
+ * whole. O = softmax(softmax_scale * Q . K) V over them, 0 for a row that sees
+ * none. bf16 MFMA products, fp32 accumulation and statistics, bf16 output.
+ *
+ * kv_len, q_start: device int32 [streams], [streams + 1], q_start ascending.
+ * Lengths past the table's width are cut to it. Of the block table only the
+ * entries of visible keys are read; their pages must be the stream's (a value
+ * outside the pool reads some page of it). max_q: the longest stream's rows,
+ * an estimate that only chooses the kernel. softmax_scale <= 0 selects
+ * 1/sqrt(128). O: Q's strides; rows of no stream are left as they were.
+ * workspace: as queried (NULL if 0), 256-byte aligned. Results do not depend
+ * on the run: partial results are merged in a fixed order.
+ * Errors: FVA_ERR_INVALID_ARG (NULL or misaligned pointers, negative max_q,
+ * frame or window, scale), FVA_ERR_SHAPE (batch != 1, heads not a multiple of
+ * the cache's, overlapping rows), FVA_ERR_UNSUPPORTED (head_dim, page,
+ * table_width * page >= 2^30, 2^31 rows or work items), FVA_ERR_WORKSPACE.
+ */
+fva_status fva_attn_cache(const void* Q, const fva_qkv_desc* q_desc, const fva_cache* cache,
+                          const int32_t* block_table, int32_t table_width, const int32_t* kv_len,
+                          const int32_t* q_start, int32_t streams, int32_t max_q, int32_t frame, int32_t window,
+                          float softmax_scale, void* O, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Static description of a status code. */
 const char* fva_status_string(fva_status status);

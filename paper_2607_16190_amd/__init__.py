@@ -17,6 +17,15 @@ attend with the one-dimensional tiling, and permute O back:
     tc = fva.Tiling.curve(21 * 45 * 80, 128)
     oc = fva.fva_attn(qc, kc, vc, tc, *fva.fva_route(qc, kc, 0.9, 4, tc))
     out = fva.fva_permute_tokens(oc, perm, fva.FVA_FROM_CURVE)
+
+Rotary positions of Q and K before routing, and a step of video that is generated in pieces over
+a paged 8-bit cache (q, k, v [1, heads, tokens, 128], the streams' new tokens packed):
+
+    q, k = fva.fva_rope(q, k, (45, 80), (44, 42, 42))
+    kv_len, q_start, slots, ids, state = fva.fva_cache_plan(held, fresh, state, ring, table, 64, tokens)
+    q, k = fva.fva_rope(q, k, (45, 80), (44, 42, 42), ids=ids)
+    fva.fva_cache_store(k, v, slots, k8, v8, k_exp, v_exp)
+    out = fva.fva_attn_cache(q, k8, v8, k_exp, v_exp, table, kv_len, q_start, max_q, frame=45 * 80)
 """
 
 import ctypes
@@ -47,6 +56,13 @@ FVA_SCHED_UNPAIRED = 4
 FVA_TO_CURVE = 0
 FVA_FROM_CURVE = 1
 
+FVA_BF16 = 0
+FVA_FP16 = 1
+FVA_FP32 = 2
+
+FVA_ROPE_PAIRS = 0
+FVA_ROPE_HALVES = 1
+
 
 def FVA_SPLIT_BLOCKS(s: int) -> int:
     """Flag bits forcing chunks of at most s kept blocks per split row (persistent scheduler)."""
@@ -69,6 +85,11 @@ EXPORTED = (
     "fva_quantize_v",
     "fva_attn_fp8v",
     "fva_attn_noalloc",
+    "fva_rope",
+    "fva_cache_plan",
+    "fva_cache_store",
+    "fva_attn_cache_workspace_size",
+    "fva_attn_cache",
     "fva_status_string",
 )
 
@@ -86,6 +107,20 @@ class _Desc(ctypes.Structure):
         ("stride_b", ctypes.c_int64),
         ("stride_h", ctypes.c_int64),
         ("stride_n", ctypes.c_int64),
+    ]
+
+
+class _RopeParams(ctypes.Structure):
+    _fields_ = [
+        *((n, ctypes.c_int32) for n in ("H", "W", "dim_t", "dim_y", "dim_x", "t0", "y0", "x0", "pairing", "inverse")),
+        ("theta", ctypes.c_double),
+    ]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [
+        *((n, ctypes.c_int32) for n in ("pages", "heads", "page", "head_dim")),
+        *((n, ctypes.c_void_p) for n in ("k8", "v8", "k_exp", "v_exp")),
     ]
 
 
@@ -162,6 +197,24 @@ def _load():
         "fva_attn_noalloc": (
             ctypes.c_int,
             [P, P, P, D, T, P, P, ctypes.c_float, ctypes.c_uint32, P, P, P],
+        ),
+        "fva_rope": (
+            ctypes.c_int,
+            [P, P, D, P, P, D, ctypes.c_int32, ctypes.POINTER(_RopeParams), P, ctypes.c_int64, P],
+        ),
+        "fva_cache_plan": (
+            ctypes.c_int,
+            [P, P, ctypes.c_int32, ctypes.c_int32, P, P, ctypes.c_int32, P, ctypes.c_int32, ctypes.c_int32, P, P, P, P,
+             P, P],
+        ),
+        "fva_cache_store": (ctypes.c_int, [P, P, D, P, ctypes.POINTER(_Cache), P]),
+        "fva_attn_cache_workspace_size": (
+            ctypes.c_int, [D, ctypes.POINTER(_Cache), ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, sz],
+        ),
+        "fva_attn_cache": (
+            ctypes.c_int,
+            [P, D, ctypes.POINTER(_Cache), P, ctypes.c_int32, P, P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+             ctypes.c_int32, ctypes.c_float, P, P, ctypes.c_size_t, P],
         ),
         "fva_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     }
@@ -452,3 +505,165 @@ def fva_attn_fp8v(q, k, v8, vexp, tiling: Tiling, mask, counts=None, kv_idx=None
     _check(st, "fva_attn_fp8v")
     return out
 
+
+
+_DTYPES = {torch.bfloat16: FVA_BF16, torch.float16: FVA_FP16, torch.float32: FVA_FP32}
+
+
+def _same_device(x, *others):
+    """The calls below run on the current device: tensors of another one are refused."""
+    if not x.is_cuda or x.device.index != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current device")
+    for t in others:
+        if t is not None and t.device != x.device:
+            raise ValueError("tensors must be on one device")
+
+
+def _int32(t, what, *shape):
+    if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise ValueError(f"{what} must be a contiguous int32 tensor of shape {shape}")
+
+
+def _empty(make, stream):
+    """make() with its memory on the stream that the call runs on, so that a freed buffer is not
+    handed to another stream while the call still uses it."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
+
+
+def fva_rope(q, k, hw, dims, *, ids=None, origin=(0, 0, 0), theta: float = 10000.0, pairing: int = FVA_ROPE_PAIRS,
+             inverse: bool = False, out=None, stream=None):
+    """Rotary positions on three axes (see include/fva.h): q and k (or None) [batch, heads, tokens, 128] turned.
+
+    hw: rows and columns of a frame; dims: channels turned by (t, y, x); ids: int32 [tokens] or [batch, tokens]
+    token ids, or None for raster order; inverse: the gradient's direction; out: the tensor(s) written, which may be
+    the inputs. Returns q turned, or (q, k) turned.
+    """
+    if q.dtype not in _DTYPES or (k is not None and k.dtype != q.dtype):
+        raise ValueError("q and k must share one of bf16, fp16 and fp32")
+    _same_device(q, k, ids)
+    xs = (q,) if k is None else (q, k)
+    if out is None:
+        out = _empty(lambda: tuple(torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device) for x in xs), stream)
+    else:
+        out = (out,) if k is None else tuple(out)
+        for x, y in zip(xs, out):
+            if y.stride() != x.stride() or y.shape != x.shape or y.dtype != x.dtype or y.device != x.device:
+                raise ValueError("out must match its input in shape, strides, dtype and device")
+    qd = _desc_of(q)
+    kd = None if k is None else _desc_of(k)
+    if kd is not None and (kd.batch != qd.batch or kd.tokens != qd.tokens):
+        raise ValueError("q and k must share batch and tokens")
+    ids_stride = 0
+    if ids is not None:
+        _int32(ids, "ids", *((qd.tokens,) if ids.dim() == 1 else (qd.batch, qd.tokens)))
+        ids_stride = 0 if ids.dim() == 1 else qd.tokens
+    params = _RopeParams(int(hw[0]), int(hw[1]), int(dims[0]), int(dims[1]), int(dims[2]), int(origin[0]),
+                         int(origin[1]), int(origin[2]), int(pairing), int(bool(inverse)), float(theta))
+    st = lib.fva_rope(
+        _ptr(q), _ptr(out[0]), ctypes.byref(qd), _ptr(k), None if k is None else _ptr(out[1]),
+        None if kd is None else ctypes.byref(kd), _DTYPES[q.dtype], ctypes.byref(params), _ptr(ids), ids_stride,
+        _stream_ptr(stream),
+    )
+    _check(st, "fva_rope")
+    return out[0] if k is None else out
+
+
+def fva_cache_plan(held, fresh, state, ring, block_table, page: int, tokens: int, *, out=None, stream=None):
+    """Pages, slots and positions of the streams' new tokens (see include/fva.h); block_table and ring change in place.
+
+    held, fresh: int32 [streams]; state: int32 [3]; ring: int32 [ring size]; block_table: int32 [streams, width];
+    tokens: rows of the slots and ids. Returns (kv_len, q_start, slots, ids, state).
+    """
+    _same_device(held, fresh, state, ring, block_table)
+    n = held.shape[0] if held.dim() == 1 else -1
+    _int32(held, "held", n)
+    _int32(fresh, "fresh", n)
+    _int32(state, "state", 3)
+    _int32(ring, "ring", ring.numel())
+    _int32(block_table, "block_table", n, block_table.shape[-1])
+    shapes = (n,), (n + 1,), (int(tokens),), (int(tokens),), (3,)
+    if out is None:
+        out = _empty(lambda: tuple(torch.empty(s, dtype=torch.int32, device=held.device) for s in shapes), stream)
+    else:
+        _same_device(held, *out)
+        for t, s, what in zip(out, shapes, ("kv_len", "q_start", "slots", "ids", "state_out")):
+            _int32(t, what, *s)
+    st = lib.fva_cache_plan(
+        _ptr(held), _ptr(fresh), n, int(page), _ptr(state), _ptr(ring), ring.numel(), _ptr(block_table),
+        block_table.shape[1], int(tokens), *map(_ptr, out), _stream_ptr(stream),
+    )
+    _check(st, "fva_cache_plan")
+    return tuple(out)
+
+
+def _cache_of(k8, v8, k_exp, v_exp) -> _Cache:
+    for t in (k8, v8):
+        if t.dtype != torch.uint8 or t.dim() != 4 or not t.is_contiguous() or t.shape != k8.shape:
+            raise ValueError("k8 and v8 must be contiguous uint8 tensors [pages, heads, page, 128]")
+    pages, heads, page, d = k8.shape
+    _int32(k_exp, "k_exp", pages, heads)
+    _int32(v_exp, "v_exp", pages, heads)
+    return _Cache(pages, heads, page, d, k8.data_ptr(), v8.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr())
+
+
+def fva_cache_store(k, v, slots, k8, v8, k_exp, v_exp, *, stream=None):
+    """K and V rows into the cache's slots, in place (see include/fva.h).
+
+    k, v: bf16 [batch, heads, tokens, 128]; slots: int32, one per (batch, token); k8, v8: uint8 [pages, heads, page,
+    128]; k_exp, v_exp: int32 [pages, heads].
+    """
+    if k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
+        raise ValueError("k and v must be bf16")
+    if k.shape != v.shape or k.stride() != v.stride():
+        raise ValueError("k and v must share shape and strides")
+    _same_device(k, v, slots, k8, v8, k_exp, v_exp)
+    desc = _desc_of(k)
+    if slots.dtype != torch.int32 or not slots.is_contiguous() or slots.numel() != desc.batch * desc.tokens:
+        raise ValueError("slots must be a contiguous int32 tensor with one entry per (batch, token)")
+    cache = _cache_of(k8, v8, k_exp, v_exp)
+    st = lib.fva_cache_store(_ptr(k), _ptr(v), ctypes.byref(desc), _ptr(slots), ctypes.byref(cache), _stream_ptr(stream))
+    _check(st, "fva_cache_store")
+
+
+def fva_attn_cache_workspace_size(desc: _Desc, cache: _Cache, table_width: int, streams: int, max_q: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(
+        lib.fva_attn_cache_workspace_size(ctypes.byref(desc), ctypes.byref(cache), int(table_width), int(streams),
+                                          int(max_q), ctypes.byref(n)),
+        "fva_attn_cache_workspace_size",
+    )
+    return n.value
+
+
+def fva_attn_cache(q, k8, v8, k_exp, v_exp, block_table, kv_len, q_start, max_q: int, *, frame: int = 0,
+                   window: int = 0, scale: float = 0.0, out=None, workspace=None, stream=None):
+    """Attention of the streams' newest tokens over their cached ones (see include/fva.h). Returns O.
+
+    q: bf16 [1, heads, tokens, 128], the streams' rows packed as q_start says; block_table: int32 [streams, width];
+    kv_len: int32 [streams]; q_start: int32 [streams + 1]; max_q: the longest stream's rows.
+    """
+    if q.dtype != torch.bfloat16:
+        raise ValueError("q must be bf16")
+    _same_device(q, k8, v8, k_exp, v_exp, block_table, kv_len, q_start, out, workspace)
+    desc = _desc_of(q)
+    cache = _cache_of(k8, v8, k_exp, v_exp)
+    n = kv_len.numel()
+    _int32(kv_len, "kv_len", n)
+    _int32(q_start, "q_start", n + 1)
+    _int32(block_table, "block_table", n, block_table.shape[-1])
+    if out is None:
+        out = _empty(lambda: torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=q.device), stream)
+    elif out.stride() != q.stride() or out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must match q in shape, strides and dtype")
+    nbytes = fva_attn_cache_workspace_size(desc, cache, block_table.shape[1], n, max_q)
+    ws = _empty(lambda: _workspace(nbytes, q.device, workspace), stream) if nbytes or workspace is not None else None
+    st = lib.fva_attn_cache(
+        _ptr(q), ctypes.byref(desc), ctypes.byref(cache), _ptr(block_table), block_table.shape[1], _ptr(kv_len),
+        _ptr(q_start), n, int(max_q), int(frame), int(window), ctypes.c_float(scale), _ptr(out), _ptr(ws),
+        0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(stream),
+    )
+    _check(st, "fva_attn_cache")
+    return out

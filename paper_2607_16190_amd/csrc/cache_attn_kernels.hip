@@ -1,0 +1,479 @@
+// Attention over the paged 8-bit K/V cache (gfx950).
+//
+// Query row i of a stream (position p = kv_len - q_len + i) of head h sees the keys
+// j in [lo, hi) of its stream,
+//     end = kv_len without frames, else (floor(p / frame) + 1) * frame,
+//     hi = min(end, kv_len), lo = max(0, end - window) with a window, else 0,
+//     O = sum_j softmax_j(scale * Q . K_j) V_j,  K_j = code * 2^ke, V_j = code * 2^ve.
+//
+// Rows are taken per K/V head: the heads / kv_heads query heads that share a K/V head lie
+// next to each other, row = token * group + head in the group, in tiles of kRows rows.
+// Work item = (tile, chunk of its keys), one workgroup per item and K/V head. The chunk
+// length follows from the lengths on the device (make_split), the same in every wave of
+// both kernels: as many items as the chip holds workgroups, where the tiles alone are
+// fewer. A tile in several chunks leaves unnormalised partial results that
+// cache_combine_kernel merges in chunk order (no atomics: the result is the same on
+// every run).
+//
+// Codes become bf16 exactly (E4M3 has four significant bits), times the page's power of
+// two in the same instruction; products are bf16 with fp32 accumulation, statistics and
+// sums fp32. P is rounded to bf16 for its product with V, as the matrix unit takes it: at
+// most half a step, 2^-9, of each term, the same as the output's own rounding.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "fva_common.h"
+#include "fva_geometry.h"
+#include "fva_internal.h"
+
+namespace fva {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kRows = 16;        // query rows of a tile (one MFMA column each)
+constexpr int kKeys = 64;        // keys a wave takes at a time
+constexpr int kWaves = 4;        // waves of a workgroup, each on every fourth 64 keys
+constexpr int kCacheSlots = 1024; // workgroups to split for: four a CU
+constexpr int kMinChunk = kWaves * kKeys;  // a shorter chunk leaves waves without keys
+constexpr int kPartial = kRows * (kHeadDim + 2);  // floats of a partial result
+
+// Integer division by a positive number, rounded up.
+__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// One stream's share of the work: its rows, keys and tiles.
+struct Stream {
+  int q0, q_len;  // first token row, tokens
+  int kv_len;
+  int tiles;
+  int span;       // keys that any of its tiles sees, at most
+};
+
+__device__ __forceinline__ Stream stream_of(const CacheAttnArgs& P, int s) {
+  Stream r;
+  // Lengths and starts come from device memory: clamped, so that no index leaves the
+  // tensors whatever they hold.
+  r.q0 = min(max(P.q_start[s], 0), P.tokens);
+  r.q_len = min(max(P.q_start[s + 1], r.q0), P.tokens) - r.q0;
+  r.kv_len = (int)min((int64_t)max(P.kv_len[s], 0), (int64_t)P.width * P.page);
+  r.tiles = (int)ceil_div((int64_t)r.q_len * P.group, kRows);
+  int64_t span = r.kv_len;
+  if (P.window) span = min(span, (int64_t)P.window + 2 * (int64_t)P.frame + kRows + kKeys);
+  r.span = (int)span;
+  return r;
+}
+
+// Which stream an item belongs to, and the chunk length.
+struct Split {
+  int chunk;
+  int stream;  // -1: no such item
+  int item0;   // first item of the stream
+};
+
+__device__ __forceinline__ int chunks_of(int span, int chunk) { return max(1, (span + chunk - 1) / chunk); }
+
+// Chunk length: with P.slots workgroups to fill per K/V head, sum over tiles of their
+// keys / slots, in whole multiples of kMinChunk. One wave, streams over lanes.
+__device__ __forceinline__ int chunk_length(const CacheAttnArgs& P, int lane) {
+  if (P.slots <= 0) return INT32_MAX / 2;
+  uint64_t total = 0;
+  for (int s = lane; s < P.streams; s += kWave) {
+    const Stream r = stream_of(P, s);
+    total += (uint64_t)r.tiles * (uint64_t)r.span;
+  }
+  total = wave_sum_u64(total);
+  const uint64_t keys = (total + P.slots - 1) / (uint64_t)P.slots;
+  const uint64_t c = (keys + kMinChunk - 1) / kMinChunk * kMinChunk;
+  return (int)min(max(c, (uint64_t)kMinChunk), (uint64_t)(INT32_MAX / 2));
+}
+
+__device__ __forceinline__ Split split_of(const CacheAttnArgs& P, int item, int lane) {
+  Split r;
+  r.chunk = chunk_length(P, lane);
+  int base = 0;
+  for (int s0 = 0; s0 < P.streams; s0 += kWave) {
+    const int s = s0 + lane;
+    int n = 0;
+    if (s < P.streams) {
+      const Stream st = stream_of(P, s);
+      n = st.tiles * chunks_of(st.span, r.chunk);
+    }
+    const int incl = wave_incl_scan_i32(n, lane);
+    const uint64_t past = __ballot(base + incl > item);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      r.stream = s0 + l;
+      r.item0 = base + __builtin_amdgcn_readlane(incl - n, l);
+      return r;
+    }
+    base += __builtin_amdgcn_readlane(incl, 63);
+  }
+  r.stream = -1;
+  r.item0 = base;
+  return r;
+}
+
+// Keys [lo, hi) that token i of a stream sees.
+__device__ __forceinline__ void visible(const CacheAttnArgs& P, const Stream& st, int i, int& lo, int& hi) {
+  const int p = st.kv_len - st.q_len + i;
+  int64_t end = st.kv_len;
+  if (P.frame) end = p < 0 ? 0 : ((int64_t)(p / P.frame) + 1) * P.frame;
+  hi = (int)min(end, (int64_t)st.kv_len);
+  lo = P.window ? (int)max(end - P.window, (int64_t)0) : 0;
+}
+
+// The keys of a tile, [begin, end) with begin on a multiple of kKeys: those that its first
+// row's window starts with to those that its last row ends with.
+struct Span {
+  int begin, lo, end;
+};
+__device__ __forceinline__ Span tile_span(const CacheAttnArgs& P, const Stream& st, int tile) {
+  const int row0 = tile * kRows;
+  const int row1 = min(row0 + kRows, st.q_len * P.group) - 1;
+  int lo, hi, lo1, hi1;
+  visible(P, st, row0 / P.group, lo, hi);
+  visible(P, st, row1 / P.group, lo1, hi1);
+  Span r;
+  r.lo = lo;
+  r.begin = lo & ~(kKeys - 1);
+  r.end = hi1 > lo ? hi1 : r.begin;  // no key at all: an empty span
+  return r;
+}
+
+// Two E4M3 codes (the low or high half of w) times a power of two, as bf16.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t two_bf16(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HIGH));
+}
+
+__device__ __forceinline__ bf16x8 eight_bf16(uint32_t lo, uint32_t hi, float scale) {
+  const uint4 r = make_uint4(two_bf16<false>(lo, scale), two_bf16<true>(lo, scale), two_bf16<false>(hi, scale),
+                             two_bf16<true>(hi, scale));
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+__device__ __forceinline__ float exp_of(int e) {  // 2^e
+  return __uint_as_float((uint32_t)(127 + min(max(e, kCacheExpMin), 120)) << 23);
+}
+
+// max over lanes l, l^16, l^32, l^48, and the sum of them.
+__device__ __forceinline__ float max4(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum4(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// One tile of query rows against one chunk of its keys.
+//
+// Operand layouts (16x16x32 products; lane = 16 g + l). S^T = K Q^T: lane (g, l) holds key
+// l of a 16-key group and channels 64 p + 16 g + 8 f .. + 7 at step 2 p + f, half of one
+// 16-byte load; Q has the same order. S^T accumulator r is key 4 g + r, query row l: with
+// two groups, the eight keys {4 g + r, 16 + 4 g + r} of a P^T operand. O^T += V^T P^T: lane
+// (g, l) needs those eight keys of a channel, so it loads 8 bytes (channels 8 l .. 8 l + 7)
+// of each of the eight rows; a byte permute of two rows' words puts two keys of one
+// channel side by side, as the conversion takes them. Tile m of O^T holds channel 8 l + m,
+// so a lane ends with eight consecutive channels of a query row per accumulator index.
+__global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_kernel(CacheAttnArgs P) {
+  __shared__ __align__(16) float ot[kWaves][kRows][kHeadDim + 4];
+  __shared__ float ms[kWaves][kRows], ls[kWaves][kRows];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, l = lane & 15;
+  const int kh = blockIdx.x % P.kv_heads;
+  const int item = blockIdx.x / P.kv_heads;
+  const Split sp = split_of(P, item, lane);
+  if (sp.stream < 0) return;
+  const Stream st = stream_of(P, sp.stream);
+  const int per_tile = chunks_of(st.span, sp.chunk);
+  const int tile = (item - sp.item0) / per_tile;
+  const int chunk = (item - sp.item0) - tile * per_tile;
+  const Span span = tile_span(P, st, tile);
+  const int n_chunks = max(1, (int)ceil_div(span.end - span.begin, sp.chunk));
+  if (chunk >= n_chunks) return;
+  const int k0 = (int)min((int64_t)span.begin + (int64_t)chunk * sp.chunk, (int64_t)span.end);
+  const int k1 = (int)min((int64_t)k0 + sp.chunk, (int64_t)span.end);
+
+  // This lane's query row.
+  const int row = tile * kRows + l;
+  const bool real = row < st.q_len * P.group;
+  const int tok = real ? row / P.group : 0;
+  const int qh = kh * P.group + (real ? row - tok * P.group : 0);
+  int lo = 0, hi = 0;
+  if (real) visible(P, st, tok, lo, hi);
+  const uint16_t* qrow = static_cast<const uint16_t*>(P.Q) + (int64_t)(st.q0 + tok) * P.stride_n + (int64_t)qh * P.stride_h;
+  bf16x8 qf[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    qf[s] = bf16x8{};
+    if (real) qf[s] = *reinterpret_cast<const bf16x8*>(qrow + 64 * (s >> 1) + 16 * g + 8 * (s & 1));
+  }
+  // Keys that every real row sees, for which nothing is masked.
+  int all_lo = real ? lo : 0, all_hi = real ? hi : INT32_MAX;
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) {
+    all_lo = max(all_lo, __shfl_xor(all_lo, d));
+    all_hi = min(all_hi, __shfl_xor(all_hi, d));
+  }
+  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+
+  const int32_t* table = P.table + (int64_t)sp.stream * P.width;
+  const float c2 = P.scale * 1.44269504088896340736f;
+  f32x4 o[8];
+#pragma unroll
+  for (int m = 0; m < 8; ++m) o[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float mref = -1.0e30f, lsum = 0.f;
+
+  for (int base = k0 + wave * kKeys; base < k1; base += kWaves * kKeys) {
+    // Keys outside [span.lo, k1) repeat the nearest one inside: their pages may be no
+    // longer the stream's, and their codes anything.
+    uint4 kraw[4][2];
+    uint2 vraw[4][4];
+    float ke[4], ve[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int first = min(max(base + 16 * t, span.lo), k1 - 1);
+      const int entry = __builtin_amdgcn_readfirstlane(min(max(table[first >> P.page_shift], 0), P.pages - 1));
+      const int64_t at = (int64_t)entry * P.kv_heads + kh;
+      ke[t] = exp_of(P.k_exp[at]);
+      ve[t] = exp_of(P.v_exp[at]);
+      const uint8_t* kp = P.k8 + at * P.page * kHeadDim;
+      const uint8_t* vp = P.v8 + at * P.page * kHeadDim;
+      const int kr = min(max(base + 16 * t + l, span.lo), k1 - 1) & (P.page - 1);
+      kraw[t][0] = *reinterpret_cast<const uint4*>(kp + kr * kHeadDim + 16 * g);
+      kraw[t][1] = *reinterpret_cast<const uint4*>(kp + kr * kHeadDim + 64 + 16 * g);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int vr = min(max(base + 16 * t + 4 * g + r, span.lo), k1 - 1) & (P.page - 1);
+        vraw[t][r] = *reinterpret_cast<const uint2*>(vp + vr * kHeadDim + 8 * l);
+      }
+    }
+    f32x4 s[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_bf16(kraw[t][p].x, kraw[t][p].y, ke[t]), qf[2 * p], s[t], 0, 0, 0);
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_bf16(kraw[t][p].z, kraw[t][p].w, ke[t]), qf[2 * p + 1], s[t], 0, 0, 0);
+      }
+    }
+    if (base < all_lo || base + kKeys > min(all_hi, k1)) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int key = base + 16 * t + 4 * g + r;
+          if (key < lo || key >= min(hi, k1)) s[t][r] = -INFINITY;
+        }
+      }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[t][r]);
+    }
+    // Running reference in units of exp2's argument; it moves where a row's maximum has
+    // passed it.
+    mx = max4(mx) * c2;
+    const float to = fmaxf(mref, mx);
+    if (__ballot(to > mref)) {
+      const float alpha = __builtin_amdgcn_exp2f(mref - to);
+#pragma unroll
+      for (int m = 0; m < 8; ++m) o[m] *= alpha;
+      lsum *= alpha;
+      mref = to;
+    }
+    bf16x8 pb[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      f32x8 e;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        e[j] = __builtin_amdgcn_exp2f(fmaf(s[2 * b + (j >> 2)][j & 3], c2, -mref));
+        lsum += e[j];
+      }
+      pb[b] = __builtin_convertvector(e, bf16x8);
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        // byte pairs of rows (2 j, 2 j + 1): channels 4 w, 4 w + 1 and 4 w + 2, 4 w + 3
+        uint32_t lo2[4], hi2[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint2 ra = vraw[2 * b + (j >> 1)][2 * (j & 1)], rb = vraw[2 * b + (j >> 1)][2 * (j & 1) + 1];
+          const uint32_t a = w ? ra.y : ra.x, c = w ? rb.y : rb.x;
+          lo2[j] = __builtin_amdgcn_perm(c, a, 0x05010400u);
+          hi2[j] = __builtin_amdgcn_perm(c, a, 0x07030602u);
+        }
+        const float e0 = ve[2 * b], e1 = ve[2 * b + 1];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t(&src)[4] = q < 2 ? lo2 : hi2;
+          uint4 f;
+          if (q & 1)
+            f = make_uint4(two_bf16<true>(src[0], e0), two_bf16<true>(src[1], e0), two_bf16<true>(src[2], e1), two_bf16<true>(src[3], e1));
+          else
+            f = make_uint4(two_bf16<false>(src[0], e0), two_bf16<false>(src[1], e0), two_bf16<false>(src[2], e1), two_bf16<false>(src[3], e1));
+          const int m = 4 * w + q;
+          o[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pb[b], o[m], 0, 0, 0);
+        }
+      }
+    }
+  }
+  lsum = sum4(lsum);
+  // The waves' results side by side: accumulator r of tile m is channel 8 (4 g + r) + m of row l.
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    *reinterpret_cast<f32x4*>(&ot[wave][l][32 * g + 8 * r]) = f32x4{o[0][r], o[1][r], o[2][r], o[3][r]};
+    *reinterpret_cast<f32x4*>(&ot[wave][l][32 * g + 8 * r + 4]) = f32x4{o[4][r], o[5][r], o[6][r], o[7][r]};
+  }
+  if (g == 0) {
+    ms[wave][l] = mref;
+    ls[wave][l] = lsum;
+  }
+  __syncthreads();
+  // Thread: row threadIdx / 16, channels 8 (threadIdx % 16) .. + 7.
+  const int orow = threadIdx.x >> 4, oc = 8 * (threadIdx.x & 15);
+  const int out_row = tile * kRows + orow;
+  if (out_row >= st.q_len * P.group) return;
+  float m = ms[0][orow];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) m = fmaxf(m, ms[w][orow]);
+  float sum = 0.f;
+  f32x8 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float f = __builtin_amdgcn_exp2f(ms[w][orow] - m);
+    sum += f * ls[w][orow];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] += f * ot[w][orow][oc + e];
+  }
+  if (n_chunks == 1) {
+    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+    const int ot_tok = out_row / P.group;
+    const int oh = kh * P.group + out_row - ot_tok * P.group;
+    uint16_t* dst = static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + ot_tok) * P.stride_n + (int64_t)oh * P.stride_h + oc;
+    *reinterpret_cast<bf16x8*>(dst) = __builtin_convertvector(acc * inv, bf16x8);
+  } else {
+    float* part = P.partial + (int64_t)blockIdx.x * kPartial;
+    *reinterpret_cast<f32x8*>(part + orow * kHeadDim + oc) = acc;
+    if (oc == 0) {
+      part[kRows * kHeadDim + orow] = m;
+      part[kRows * kHeadDim + kRows + orow] = sum;
+    }
+  }
+}
+
+// One wave per query row: the partial results of its tile's chunks, in chunk order.
+__global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
+  const int lane = threadIdx.x & 63;
+  const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = (int)(id / P.heads), h = (int)(id % P.heads);
+  if (n >= P.tokens) return;
+  const int chunk = chunk_length(P, lane);
+  // the stream that holds token row n, and its first item
+  int base = 0, stream = -1, item0 = 0;
+  for (int s0 = 0; s0 < P.streams; s0 += kWave) {
+    const int s = s0 + lane;
+    int cnt = 0;
+    bool holds = false;
+    if (s < P.streams) {
+      const Stream st = stream_of(P, s);
+      cnt = st.tiles * chunks_of(st.span, chunk);
+      holds = n >= st.q0 && n < st.q0 + st.q_len;
+    }
+    const int incl = wave_incl_scan_i32(cnt, lane);
+    const uint64_t at = __ballot(holds);
+    if (at) {
+      const int l = __builtin_ctzll(at);
+      stream = s0 + l;
+      item0 = base + __builtin_amdgcn_readlane(incl - cnt, l);
+      break;
+    }
+    base += __builtin_amdgcn_readlane(incl, 63);
+  }
+  if (stream < 0) return;
+  const Stream st = stream_of(P, stream);
+  const int kh = h / P.group;
+  const int row = (n - st.q0) * P.group + h - kh * P.group;
+  const int tile = row / kRows, r = row - tile * kRows;
+  const Span span = tile_span(P, st, tile);
+  const int n_chunks = max(1, (int)ceil_div(span.end - span.begin, chunk));
+  if (n_chunks == 1) return;
+  const int64_t first = (int64_t)(item0 + tile * chunks_of(st.span, chunk)) * P.kv_heads + kh;
+  if (first + (int64_t)(n_chunks - 1) * P.kv_heads >= P.items) return;  // starts that are not ascending
+  float m = -1.0e30f, sum = 0.f;
+  float2 acc = make_float2(0.f, 0.f);
+  for (int c = 0; c < n_chunks; ++c) {
+    const float* part = P.partial + (first + (int64_t)c * P.kv_heads) * kPartial;
+    const float pm = part[kRows * kHeadDim + r], pl = part[kRows * kHeadDim + kRows + r];
+    const float2 po = *reinterpret_cast<const float2*>(part + r * kHeadDim + 2 * lane);
+    const float to = fmaxf(m, pm);
+    const float a = __builtin_amdgcn_exp2f(m - to), b = __builtin_amdgcn_exp2f(pm - to);
+    acc.x = acc.x * a + po.x * b;
+    acc.y = acc.y * a + po.y * b;
+    sum = sum * a + pl * b;
+    m = to;
+  }
+  const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+  bf16x2 v;
+  v[0] = (__bf16)(acc.x * inv);
+  v[1] = (__bf16)(acc.y * inv);
+  *reinterpret_cast<bf16x2*>(static_cast<uint16_t*>(P.O) + (int64_t)n * P.stride_n + (int64_t)h * P.stride_h + 2 * lane) = v;
+}
+
+// Workgroups per K/V head to fill (0: the tiles alone do), and the items there can be.
+struct Sizes {
+  int slots;
+  int64_t items;
+};
+Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int64_t most_keys) {
+  const int group = heads / kv_heads;
+  const int64_t tiles = (int64_t)tokens * group / kRows + streams;  // at most one partly filled tile a stream
+  Sizes r;
+  r.slots = std::max(1, kCacheSlots / kv_heads);
+  if (most_keys <= kMinChunk || tiles >= 4 * (int64_t)r.slots) r.slots = 0;
+  r.items = tiles + r.slots;
+  return r;
+}
+
+}  // namespace
+
+int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int64_t most_keys) {
+  return sizes_of(tokens, heads, kv_heads, streams, most_keys).items * kv_heads;
+}
+
+size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int streams, int64_t most_keys) {
+  const Sizes z = sizes_of(tokens, heads, kv_heads, streams, most_keys);
+  return z.slots ? (size_t)z.items * kv_heads * kPartial * sizeof(float) : 0;
+}
+
+hipError_t launch_cache_attn(CacheAttnArgs a) {
+  (void)hipGetLastError();
+  if (a.tokens == 0 || a.heads == 0 || a.streams == 0) return hipSuccess;
+  a.group = a.heads / a.kv_heads;
+  const Sizes z = sizes_of(a.tokens, a.heads, a.kv_heads, a.streams, (int64_t)a.width * a.page);
+  a.slots = z.slots;
+  a.items = z.items * a.kv_heads;
+  cache_attn_kernel<<<(unsigned)(z.items * a.kv_heads), kWaves * kWave, 0, a.stream>>>(a);
+  if (z.slots) cache_combine_kernel<<<(unsigned)(((int64_t)a.tokens * a.heads + 3) / 4), 256, 0, a.stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace fva

@@ -88,4 +88,93 @@ hipError_t launch_curve_order(int T, int H, int W, int32_t* perm, void* workspac
 hipError_t launch_permute_rows(const void* src, void* dst, int batch, int heads, int tokens, int64_t sb, int64_t sh,
                                int64_t sn, const int32_t* perm, int direction, hipStream_t stream);
 
+// Rotary positions (rope_kernels.hip). One of Q and K; `out` may be `in`.
+struct RopeTensor {
+  const void* in = nullptr;
+  void* out = nullptr;
+  int heads = 0;
+  int64_t sb = 0, sh = 0, sn = 0;
+};
+
+struct RopeArgs {
+  RopeTensor q, k;  // k.heads == 0: Q alone
+  int dtype;        // FVA_BF16, FVA_FP16 or FVA_FP32
+  int batch, tokens;
+  int H, W, dim_t, dim_y, dim_x, t0, y0, x0;
+  double log2_theta;
+  bool halves, inverse;
+  const int32_t* ids;  // token ids, or null: 0, 1, ..
+  int64_t ids_stride;  // between batches
+  hipStream_t stream;
+};
+
+hipError_t launch_rope(const RopeArgs& a);
+
+// Paged 8-bit cache (cache_kernels.hip).
+constexpr int kPlanStreams = 2048;   // streams of a plan: their prefix sums are kept in LDS
+constexpr int kCacheExpMin = -100;   // smallest exponent of a scale: 448 * 2^-100 is far below any activation, and
+                                     // every scaled code stays a normal fp32 and bf16 number
+
+struct PlanArgs {
+  const int32_t* held;
+  const int32_t* fresh;
+  int streams, page;
+  const int32_t* state;
+  int32_t* ring;
+  int ring_size;
+  int32_t* table;
+  int width, tokens;
+  int32_t* kv_len;
+  int32_t* q_start;
+  int32_t* slots;
+  int32_t* ids;
+  int32_t* state_out;
+  hipStream_t stream;
+};
+
+struct StoreArgs {
+  const void* K;
+  const void* V;
+  int batch, heads, tokens;
+  int64_t stride_b, stride_h, stride_n;
+  const int32_t* slots;
+  uint8_t* k8;
+  uint8_t* v8;
+  int32_t* k_exp;
+  int32_t* v_exp;
+  int pages, page;
+  int window = 0;  // token rows a wave looks through for the runs it stores
+  hipStream_t stream;
+};
+
+struct CacheAttnArgs {
+  const void* Q;
+  void* O;
+  int heads, kv_heads, tokens;
+  int64_t stride_h, stride_n;
+  const uint8_t* k8;
+  const uint8_t* v8;
+  const int32_t* k_exp;
+  const int32_t* v_exp;
+  int pages, page, page_shift;
+  const int32_t* table;
+  int width;
+  const int32_t* kv_len;
+  const int32_t* q_start;
+  int streams, max_q, frame, window;
+  float scale;
+  float* partial;
+  hipStream_t stream;
+  // set by the launcher
+  int group = 1;       // query heads per K/V head
+  int slots = 0;       // workgroups per K/V head that the keys are split for; 0: not split
+  int64_t items = 0;   // partial results there is room for
+};
+
+hipError_t launch_cache_plan(const PlanArgs& a);
+hipError_t launch_cache_store(StoreArgs a);
+int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int64_t most_keys);
+size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int streams, int64_t most_keys);
+hipError_t launch_cache_attn(CacheAttnArgs a);
+
 }  // namespace fva

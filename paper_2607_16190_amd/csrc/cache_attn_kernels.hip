@@ -23,6 +23,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "fva_common.h"
 #include "fva_geometry.h"
@@ -32,16 +33,19 @@ namespace fva {
 namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kRows = 16;        // query rows of a tile (one MFMA column each)
+constexpr int kRows = 16;        // query rows of a small tile: one MFMA column each
+constexpr int kBigRows = 128;    // query rows of a large tile: 32 for each wave
 constexpr int kKeys = 64;        // keys a wave takes at a time
 constexpr int kWaves = 4;        // waves of a workgroup, each on every fourth 64 keys
-constexpr int kCacheSlots = 1024; // workgroups to split for: four a CU
+constexpr int kCacheSlots = 1024; // workgroups to split for, small tiles: four a CU
+constexpr int kBigSlots = 512;    // large tiles: two a CU, as many as are resident
+constexpr int kXcds = 8;
 constexpr int kMinChunk = kWaves * kKeys;  // a shorter chunk leaves waves without keys
-constexpr int kPartial = kRows * (kHeadDim + 2);  // floats of a partial result
 
 // Integer division by a positive number, rounded up.
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -61,9 +65,9 @@ __device__ __forceinline__ Stream stream_of(const CacheAttnArgs& P, int s) {
   r.q0 = min(max(P.q_start[s], 0), P.tokens);
   r.q_len = min(max(P.q_start[s + 1], r.q0), P.tokens) - r.q0;
   r.kv_len = (int)min((int64_t)max(P.kv_len[s], 0), (int64_t)P.width * P.page);
-  r.tiles = (int)ceil_div((int64_t)r.q_len * P.group, kRows);
+  r.tiles = (int)((((int64_t)r.q_len * P.group) + P.rows - 1) >> P.row_shift);
   int64_t span = r.kv_len;
-  if (P.window) span = min(span, (int64_t)P.window + 2 * (int64_t)P.frame + kRows + kKeys);
+  if (P.window) span = min(span, (int64_t)P.window + 2 * (int64_t)P.frame + P.rows + kKeys);
   r.span = (int)span;
   return r;
 }
@@ -118,6 +122,18 @@ __device__ __forceinline__ Split split_of(const CacheAttnArgs& P, int item, int 
   return r;
 }
 
+// All items of a call, per K/V head.
+__device__ __forceinline__ int total_items(const CacheAttnArgs& P, int lane) {
+  const int chunk = chunk_length(P, lane);
+  uint64_t n = 0;
+  for (int s = lane; s < P.streams; s += kWave) {
+    const Stream st = stream_of(P, s);
+    n += (uint64_t)st.tiles * (uint64_t)chunks_of(st.span, chunk);
+  }
+  // (starts that are not ascending could ask for more than there is room for)
+  return (int)min(wave_sum_u64(n), (uint64_t)(P.items / P.kv_heads));
+}
+
 // Keys [lo, hi) that token i of a stream sees.
 __device__ __forceinline__ void visible(const CacheAttnArgs& P, const Stream& st, int i, int& lo, int& hi) {
   const int p = st.kv_len - st.q_len + i;
@@ -133,8 +149,8 @@ struct Span {
   int begin, lo, end;
 };
 __device__ __forceinline__ Span tile_span(const CacheAttnArgs& P, const Stream& st, int tile) {
-  const int row0 = tile * kRows;
-  const int row1 = min(row0 + kRows, st.q_len * P.group) - 1;
+  const int row0 = tile * P.rows;
+  const int row1 = min(row0 + P.rows, st.q_len * P.group) - 1;
   int lo, hi, lo1, hi1;
   visible(P, st, row0 / P.group, lo, hi);
   visible(P, st, row1 / P.group, lo1, hi1);
@@ -371,11 +387,311 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_kernel(CacheAttn
     uint16_t* dst = static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + ot_tok) * P.stride_n + (int64_t)oh * P.stride_h + oc;
     *reinterpret_cast<bf16x8*>(dst) = __builtin_convertvector(acc * inv, bf16x8);
   } else {
-    float* part = P.partial + (int64_t)blockIdx.x * kPartial;
+    float* part = P.partial + ((int64_t)item * P.kv_heads + kh) * (kRows * (kHeadDim + 2));
     *reinterpret_cast<f32x8*>(part + orow * kHeadDim + oc) = acc;
     if (oc == 0) {
       part[kRows * kHeadDim + orow] = m;
       part[kRows * kHeadDim + kRows + orow] = sum;
+    }
+  }
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) unsigned char lds_u8;
+typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+
+template <int B, int E, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (B < E) {
+    f(std::integral_constant<int, B>{});
+    static_for<B + 1, E>(f);
+  }
+}
+
+// A large tile: 128 query rows, 32 per wave, against one chunk of its keys, 64 at a time.
+//
+// The 64 keys' codes are read once for the workgroup (two 16-byte pieces of K and of V per
+// thread, while the 64 before them are multiplied), become bf16 in registers and go to
+// LDS, where all four waves read them: a conversion is paid once for 128 rows. LDS holds
+// two such steps. Rows of 256 bytes; K's 16-byte chunk c of row r lies at c ^ r % 16, V's
+// at c ^ 2 (r % 8): the reads of both products are free of bank conflicts.
+//
+// Bound by the matrix and vector units together (64 + 4 products of 16 passes a wave and
+// step against 32 exponentials and their arguments, maxima and conversions).
+__global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(CacheAttnArgs P) {
+  constexpr int NT = 2;
+  constexpr int kRow = 256;
+  constexpr int kTile = kKeys * kRow;
+  __shared__ __align__(16) unsigned char lds[4 * kTile];  // K, K of the next step, V, V
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, l = lane & 15;
+
+  // Work items head by head, the runs of consecutive ones on one XCD (workgroups go to the
+  // XCDs in turn): the tiles of a head read its keys out of one L2. Later tiles first: with
+  // causal frames they see the most keys.
+  const int total = total_items(P, lane);
+  const int64_t all = (int64_t)total * P.kv_heads;
+  const int64_t run = (all + kXcds - 1) / kXcds;
+  const int64_t index = (blockIdx.x % kXcds) * run + blockIdx.x / kXcds;
+  if (blockIdx.x / kXcds >= run || index >= all) return;
+  const int kh = (int)(index / total);
+  const int item = total - 1 - (int)(index - (int64_t)kh * total);
+  const Split sp = split_of(P, item, lane);
+  if (sp.stream < 0) return;
+  const Stream st = stream_of(P, sp.stream);
+  const int per_tile = chunks_of(st.span, sp.chunk);
+  const int tile = (item - sp.item0) / per_tile;
+  const int chunk = (item - sp.item0) - tile * per_tile;
+  const Span span = tile_span(P, st, tile);
+  const int n_chunks = max(1, (int)ceil_div(span.end - span.begin, sp.chunk));
+  if (chunk >= n_chunks) return;
+  const int k0 = (int)min((int64_t)span.begin + (int64_t)chunk * sp.chunk, (int64_t)span.end);
+  const int k1 = (int)min((int64_t)k0 + sp.chunk, (int64_t)span.end);
+
+  const int rows = st.q_len * P.group;
+  const int row0 = tile * kBigRows + 32 * wave;
+  int lo[NT], hi[NT];
+  int wave_lo = INT32_MAX, wave_hi = 0, all_lo = 0, all_hi = INT32_MAX;
+  bf16x8 qf[NT][4];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = row0 + 16 * nt + l;
+    lo[nt] = hi[nt] = 0;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) qf[nt][ks] = bf16x8{};
+    if (row < rows) {
+      const int tok = row / P.group;
+      const int qh = kh * P.group + row - tok * P.group;
+      visible(P, st, tok, lo[nt], hi[nt]);
+      const uint16_t* q = static_cast<const uint16_t*>(P.Q) + (int64_t)(st.q0 + tok) * P.stride_n + (int64_t)qh * P.stride_h;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) qf[nt][ks] = *reinterpret_cast<const bf16x8*>(q + 32 * ks + 8 * g);
+      all_lo = max(all_lo, lo[nt]);
+      all_hi = min(all_hi, hi[nt]);
+      if (hi[nt] > lo[nt]) {
+        wave_lo = min(wave_lo, lo[nt]);
+        wave_hi = max(wave_hi, hi[nt]);
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) {
+    all_lo = max(all_lo, __shfl_xor(all_lo, d));
+    all_hi = min(all_hi, __shfl_xor(all_hi, d));
+    wave_lo = min(wave_lo, __shfl_xor(wave_lo, d));
+    wave_hi = max(wave_hi, __shfl_xor(wave_hi, d));
+  }
+  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  all_hi = min(__builtin_amdgcn_readfirstlane(all_hi), k1);
+  wave_lo = __builtin_amdgcn_readfirstlane(wave_lo);
+  wave_hi = min(__builtin_amdgcn_readfirstlane(wave_hi), k1);
+
+  const int32_t* table = P.table + (int64_t)sp.stream * P.width;
+  const float c2 = P.scale * 1.44269504088896340736f;
+
+  // This thread's two pieces of a step: rows 8 wave + lane / 8 and 32 more, 16 channels
+  // from 16 (lane % 8) on. The eight rows of a wave lie in one page.
+  const int pr = lane >> 3, pc = lane & 7;
+  uint4 kraw[2], vraw[2];
+  float ke[2], ve[2];
+  auto fetch = [&](int base) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      // keys outside [span.lo, k1) repeat the nearest one inside
+      const int at = base + 32 * u + 8 * wave;
+      const int first = min(max(at, span.lo), k1 - 1);
+      const int entry = __builtin_amdgcn_readfirstlane(min(max(table[first >> P.page_shift], 0), P.pages - 1));
+      const int64_t tile_at = (int64_t)entry * P.kv_heads + kh;
+      ke[u] = exp_of(P.k_exp[tile_at]);
+      ve[u] = exp_of(P.v_exp[tile_at]);
+      const int r = min(max(at + pr, span.lo), k1 - 1) & (P.page - 1);
+      const int64_t off = tile_at * (P.page * kHeadDim) + r * kHeadDim + 16 * pc;
+      kraw[u] = *reinterpret_cast<const uint4*>(P.k8 + off);
+      vraw[u] = *reinterpret_cast<const uint4*>(P.v8 + off);
+    }
+  };
+  auto stage = [&](int buf) {
+    unsigned char* kt = lds + buf * kTile;
+    unsigned char* vt = lds + (2 + buf) * kTile;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = 32 * u + 8 * wave + pr;
+      *reinterpret_cast<bf16x8*>(kt + r * kRow + 16 * ((2 * pc) ^ (r & 15))) = eight_bf16(kraw[u].x, kraw[u].y, ke[u]);
+      *reinterpret_cast<bf16x8*>(kt + r * kRow + 16 * ((2 * pc + 1) ^ (r & 15))) = eight_bf16(kraw[u].z, kraw[u].w, ke[u]);
+      *reinterpret_cast<bf16x8*>(vt + r * kRow + 16 * ((2 * pc) ^ (2 * (r & 7)))) = eight_bf16(vraw[u].x, vraw[u].y, ve[u]);
+      *reinterpret_cast<bf16x8*>(vt + r * kRow + 16 * ((2 * pc + 1) ^ (2 * (r & 7)))) = eight_bf16(vraw[u].z, vraw[u].w, ve[u]);
+    }
+  };
+
+  f32x4 o[8][NT], lsum[NT];
+  float mrow[NT], thr[NT], negm[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int mt = 0; mt < 8; ++mt) o[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    lsum[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    mrow[nt] = thr[nt] = -1.0e30f;
+    negm[nt] = 0.f;
+  }
+  // The reference of a row moves when its maximum passes it by 2^8: P stays below 2^8,
+  // where its relative rounding is the same, and O is rarely rescaled. The sums of P come
+  // from the matrix unit too: a product with ones.
+  const float move_ref = 8.0f / c2;
+  bf16x8 ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.0f;
+
+  uint32_t kaddr[4], vaddr[8];
+  {
+    const uint32_t base = (uint32_t)(uintptr_t)(lds_u8*)lds;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) kaddr[ks] = base + l * kRow + 16 * ((4 * ks + g) ^ l);
+    // transposing reads: lane 4 e + q of group g points at row 16 hf + 4 g + e, 8-byte chunk 4 mt + q
+    const int vr = 4 * g + (l >> 2);
+#pragma unroll
+    for (int mt = 0; mt < 8; ++mt) vaddr[mt] = base + 2 * kTile + vr * kRow + 8 * (4 * (mt ^ (vr & 7)) + (l & 3));
+  }
+
+  if (k0 < k1) {
+    fetch(k0);
+    stage(0);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int base = k0; base < k1; base += kKeys) {
+    const bool more = base + kKeys < k1;
+    if (more) fetch(base + kKeys);
+    if (base < wave_hi && base + kKeys > wave_lo) {
+      auto kfrag = [&](int t, int ks) { return *(lds_bf16x8*)((lds_u8*)(uintptr_t)kaddr[ks] + buf * kTile + t * 16 * kRow); };
+      auto vfrag = [&](int kk, int mt) {
+        lds_u8* at = (lds_u8*)(uintptr_t)vaddr[mt] + buf * kTile + kk * 32 * kRow;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * kRow));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+      // S^T: step u takes key tile 2 (u / 8) + u % 2 at channels 32 (u % 8 / 2): four
+      // independent chains alternate; fragments are read two steps ahead.
+      f32x4 s[4][NT];
+      {
+        bf16x8 kq[3];
+        kq[0] = kfrag(0, 0);
+        kq[1] = kfrag(1, 0);
+        __builtin_amdgcn_s_setprio(2);
+        static_for<0, 16>([&](auto u_c) {
+          constexpr int u = decltype(u_c)::value;
+          constexpr int t = 2 * (u >> 3) + (u & 1), ks = (u & 7) >> 1;
+          if constexpr (u + 2 < 16) kq[(u + 2) % 3] = kfrag(2 * ((u + 2) >> 3) + (u & 1), ((u + 2) & 7) >> 1);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            s[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kq[u % 3], qf[nt][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t][nt], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        __builtin_amdgcn_s_setprio(0);
+      }
+      if (base < all_lo || base + kKeys > all_hi) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int key = base + 16 * t + 4 * g + r;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              if (key < lo[nt] || key >= min(hi[nt], k1)) s[t][nt][r] = -INFINITY;
+          }
+        }
+      }
+      float mx[NT];
+      bool over = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        mx[nt] = s[0][nt][0];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) mx[nt] = fmaxf(mx[nt], s[t][nt][r]);
+        }
+        over |= mx[nt] > thr[nt];
+      }
+      if (__ballot(over)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float rmx = max4(mx[nt]);
+          const bool grow = rmx > thr[nt];
+          const float to = grow ? rmx : mrow[nt];
+          const float alpha = grow ? __builtin_amdgcn_exp2f((mrow[nt] - to) * c2) : 1.0f;
+          mrow[nt] = to;
+          if (__ballot(grow)) {
+#pragma unroll
+            for (int mt = 0; mt < 8; ++mt) o[mt][nt] *= alpha;
+            lsum[nt] *= alpha;
+            thr[nt] = mrow[nt] + move_ref;
+            negm[nt] = -mrow[nt] * c2;
+          }
+        }
+      }
+      bf16x8 pb[2][NT];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          f32x8 e;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(s[2 * kk + (j >> 2)][nt][j & 3], c2, negm[nt]));
+          pb[kk][nt] = __builtin_convertvector(e, bf16x8);
+        }
+      }
+      // O^T += V^T P^T
+      {
+        bf16x8 vq[3];
+        vq[0] = vfrag(0, 0);
+        vq[1] = vfrag(0, 1);
+        __builtin_amdgcn_s_setprio(1);
+        static_for<0, 16>([&](auto u_c) {
+          constexpr int u = decltype(u_c)::value;
+          constexpr int kk = u >> 3, mt = u & 7;
+          if constexpr (u + 2 < 16) vq[(u + 2) % 3] = vfrag((u + 2) >> 3, (u + 2) & 7);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            o[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vq[u % 3], pb[kk][nt], o[mt][nt], 0, 0, 0);
+          if constexpr (mt == 7) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              lsum[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[kk][nt], lsum[nt], 0, 0, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        __builtin_amdgcn_s_setprio(0);
+      }
+    }
+    if (more) stage(buf ^ 1);
+    __syncthreads();
+    buf ^= 1;
+  }
+
+  // Accumulator r of (mt, nt): channel 16 mt + 4 g + r of row 16 nt + l.
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = row0 + 16 * nt + l;
+    if (row >= rows) continue;
+    if (n_chunks == 1) {
+      const float inv = lsum[nt][0] > 0.f ? 1.0f / lsum[nt][0] : 0.f;
+      const int tok = row / P.group;
+      const int qh = kh * P.group + row - tok * P.group;
+      uint16_t* out = static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + tok) * P.stride_n + (int64_t)qh * P.stride_h + 4 * g;
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt)
+        *reinterpret_cast<bf16x4*>(out + 16 * mt) = __builtin_convertvector(o[mt][nt] * inv, bf16x4);
+    } else {
+      float* part = P.partial + ((int64_t)item * P.kv_heads + kh) * (kBigRows * (kHeadDim + 2));
+      const int r = row - tile * kBigRows;
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt) *reinterpret_cast<f32x4*>(part + r * kHeadDim + 16 * mt + 4 * g) = o[mt][nt];
+      if (g == 0) {
+        part[kBigRows * kHeadDim + r] = mrow[nt] * c2;
+        part[kBigRows * kHeadDim + kBigRows + r] = lsum[nt][0];
+      }
     }
   }
 }
@@ -412,7 +728,7 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   const Stream st = stream_of(P, stream);
   const int kh = h / P.group;
   const int row = (n - st.q0) * P.group + h - kh * P.group;
-  const int tile = row / kRows, r = row - tile * kRows;
+  const int tile = row >> P.row_shift, r = row & (P.rows - 1);
   const Span span = tile_span(P, st, tile);
   const int n_chunks = max(1, (int)ceil_div(span.end - span.begin, chunk));
   if (n_chunks == 1) return;
@@ -421,8 +737,8 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   float m = -1.0e30f, sum = 0.f;
   float2 acc = make_float2(0.f, 0.f);
   for (int c = 0; c < n_chunks; ++c) {
-    const float* part = P.partial + (first + (int64_t)c * P.kv_heads) * kPartial;
-    const float pm = part[kRows * kHeadDim + r], pl = part[kRows * kHeadDim + kRows + r];
+    const float* part = P.partial + (first + (int64_t)c * P.kv_heads) * (P.rows * (kHeadDim + 2));
+    const float pm = part[P.rows * kHeadDim + r], pl = part[P.rows * kHeadDim + P.rows + r];
     const float2 po = *reinterpret_cast<const float2*>(part + r * kHeadDim + 2 * lane);
     const float to = fmaxf(m, pm);
     const float a = __builtin_amdgcn_exp2f(m - to), b = __builtin_amdgcn_exp2f(pm - to);
@@ -438,16 +754,22 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   *reinterpret_cast<bf16x2*>(static_cast<uint16_t*>(P.O) + (int64_t)n * P.stride_n + (int64_t)h * P.stride_h + 2 * lane) = v;
 }
 
-// Workgroups per K/V head to fill (0: the tiles alone do), and the items there can be.
+// Which kernel, the workgroups per K/V head to split for (0: the tiles alone fill the
+// device), and the items there can be.
 struct Sizes {
-  int slots;
+  bool big;
+  int rows, slots;
   int64_t items;
 };
-Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int64_t most_keys) {
+Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
   const int group = heads / kv_heads;
-  const int64_t tiles = (int64_t)tokens * group / kRows + streams;  // at most one partly filled tile a stream
   Sizes r;
-  r.slots = std::max(1, kCacheSlots / kv_heads);
+  // One small tile per stream reads the keys once, straight into registers. More rows than
+  // that share the keys' conversion through LDS in large tiles.
+  r.big = (int64_t)max_q * group > kRows;
+  r.rows = r.big ? kBigRows : kRows;
+  const int64_t tiles = (int64_t)tokens * group / r.rows + streams;  // at most one partly filled tile a stream
+  r.slots = std::max(1, (r.big ? kBigSlots : kCacheSlots) / kv_heads);
   if (most_keys <= kMinChunk || tiles >= 4 * (int64_t)r.slots) r.slots = 0;
   r.items = tiles + r.slots;
   return r;
@@ -455,23 +777,28 @@ Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int64_t most_ke
 
 }  // namespace
 
-int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int64_t most_keys) {
-  return sizes_of(tokens, heads, kv_heads, streams, most_keys).items * kv_heads;
+int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
+  return sizes_of(tokens, heads, kv_heads, streams, max_q, most_keys).items * kv_heads + kXcds;
 }
 
-size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int streams, int64_t most_keys) {
-  const Sizes z = sizes_of(tokens, heads, kv_heads, streams, most_keys);
-  return z.slots ? (size_t)z.items * kv_heads * kPartial * sizeof(float) : 0;
+size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
+  const Sizes z = sizes_of(tokens, heads, kv_heads, streams, max_q, most_keys);
+  return z.slots ? (size_t)z.items * kv_heads * z.rows * (kHeadDim + 2) * sizeof(float) : 0;
 }
 
 hipError_t launch_cache_attn(CacheAttnArgs a) {
   (void)hipGetLastError();
   if (a.tokens == 0 || a.heads == 0 || a.streams == 0) return hipSuccess;
   a.group = a.heads / a.kv_heads;
-  const Sizes z = sizes_of(a.tokens, a.heads, a.kv_heads, a.streams, (int64_t)a.width * a.page);
+  const Sizes z = sizes_of(a.tokens, a.heads, a.kv_heads, a.streams, a.max_q, (int64_t)a.width * a.page);
+  a.rows = z.rows;
+  a.row_shift = z.big ? 7 : 4;
   a.slots = z.slots;
   a.items = z.items * a.kv_heads;
-  cache_attn_kernel<<<(unsigned)(z.items * a.kv_heads), kWaves * kWave, 0, a.stream>>>(a);
+  if (z.big)
+    cache_attn_big_kernel<<<(unsigned)((a.items + kXcds - 1) / kXcds * kXcds), kWaves * kWave, 0, a.stream>>>(a);
+  else
+    cache_attn_kernel<<<(unsigned)a.items, kWaves * kWave, 0, a.stream>>>(a);
   if (z.slots) cache_combine_kernel<<<(unsigned)(((int64_t)a.tokens * a.heads + 3) / 4), 256, 0, a.stream>>>(a);
   return hipGetLastError();
 }

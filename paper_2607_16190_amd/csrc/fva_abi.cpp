@@ -431,14 +431,14 @@ fva_status check_cache(const fva_cache* c) {
 
 // Shape checks of fva_attn_cache and its workspace query.
 fva_status check_cache_attn(const fva_qkv_desc* d, int32_t kv_heads, int32_t page, int32_t table_width,
-                            int32_t streams) {
+                            int32_t streams, int32_t max_q) {
   const fva_status s = check_rows(d, 8, true);
   if (s != FVA_OK) return s;
   if (d->batch != 1 || kv_heads <= 0 || d->heads % kv_heads != 0) return FVA_ERR_SHAPE;
   if (table_width <= 0 || streams < 0) return FVA_ERR_SHAPE;
   if ((int64_t)table_width * page > INT32_MAX / 2) return FVA_ERR_UNSUPPORTED;
   if ((int64_t)d->tokens * d->heads > INT32_MAX) return FVA_ERR_UNSUPPORTED;
-  if (fva::cache_attn_items(d->tokens, d->heads, kv_heads, streams, (int64_t)table_width * page) > INT32_MAX)
+  if (fva::cache_attn_items(d->tokens, d->heads, kv_heads, streams, max_q, (int64_t)table_width * page) > INT32_MAX)
     return FVA_ERR_UNSUPPORTED;
   return FVA_OK;
 }
@@ -567,9 +567,9 @@ fva_status fva_attn_cache_workspace_size(const fva_qkv_desc* q_desc, const fva_c
   if (!bytes || max_q < 0) return FVA_ERR_INVALID_ARG;
   fva_status s = check_cache(cache);
   if (s != FVA_OK) return s;
-  s = check_cache_attn(q_desc, cache->heads, cache->page, table_width, streams);
+  s = check_cache_attn(q_desc, cache->heads, cache->page, table_width, streams, max_q);
   if (s != FVA_OK) return s;
-  *bytes = fva::cache_attn_workspace_bytes(q_desc->tokens, q_desc->heads, cache->heads, streams,
+  *bytes = fva::cache_attn_workspace_bytes(q_desc->tokens, q_desc->heads, cache->heads, streams, max_q,
                                            (int64_t)table_width * cache->page);
   return FVA_OK;
 }
@@ -582,13 +582,13 @@ fva_status fva_attn_cache(const void* Q, const fva_qkv_desc* q_desc, const fva_c
   if (std::isnan(softmax_scale) || std::isinf(softmax_scale)) return FVA_ERR_INVALID_ARG;
   fva_status s = check_cache(cache);
   if (s != FVA_OK) return s;
-  s = check_cache_attn(q_desc, cache->heads, cache->page, table_width, streams);
+  s = check_cache_attn(q_desc, cache->heads, cache->page, table_width, streams, max_q);
   if (s != FVA_OK) return s;
   if (q_desc->tokens == 0 || q_desc->heads == 0 || streams == 0) return FVA_OK;  // empty tensors have no memory
   if (!Q || !O || !block_table || !kv_len || !q_start) return FVA_ERR_INVALID_ARG;
   if (!aligned16(Q) || !aligned16(O) || !aligned4(block_table) || !aligned4(kv_len) || !aligned4(q_start))
     return FVA_ERR_INVALID_ARG;
-  const size_t need = fva::cache_attn_workspace_bytes(q_desc->tokens, q_desc->heads, cache->heads, streams,
+  const size_t need = fva::cache_attn_workspace_bytes(q_desc->tokens, q_desc->heads, cache->heads, streams, max_q,
                                                       (int64_t)table_width * cache->page);
   if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u)))
     return FVA_ERR_WORKSPACE;

@@ -167,14 +167,15 @@ struct CacheAttnArgs {
   hipStream_t stream;
   // set by the launcher
   int group = 1;       // query heads per K/V head
+  int rows = 16, row_shift = 4;  // query rows of a tile, a power of two
   int slots = 0;       // workgroups per K/V head that the keys are split for; 0: not split
   int64_t items = 0;   // partial results there is room for
 };
 
 hipError_t launch_cache_plan(const PlanArgs& a);
 hipError_t launch_cache_store(StoreArgs a);
-int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int64_t most_keys);
-size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int streams, int64_t most_keys);
+int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys);
+size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys);
 hipError_t launch_cache_attn(CacheAttnArgs a);
 
 }  // namespace fva

@@ -56,6 +56,7 @@ struct Stream {
   int kv_len;
   int tiles;
   int span;       // keys that any of its tiles sees, at most
+  int mean;       // about how many they see in the middle, at least span / 2
 };
 
 __device__ __forceinline__ Stream stream_of(const CacheAttnArgs& P, int s) {
@@ -69,6 +70,7 @@ __device__ __forceinline__ Stream stream_of(const CacheAttnArgs& P, int s) {
   int64_t span = r.kv_len;
   if (P.window) span = min(span, (int64_t)P.window + 2 * (int64_t)P.frame + P.rows + kKeys);
   r.span = (int)span;
+  r.mean = P.frame ? (int)min(span, max((int64_t)r.kv_len - (r.q_len >> 1), (int64_t)((r.kv_len + 1) >> 1))) : r.span;
   return r;
 }
 
@@ -81,19 +83,33 @@ struct Split {
 
 __device__ __forceinline__ int chunks_of(int span, int chunk) { return max(1, (span + chunk - 1) / chunk); }
 
-// Chunk length: with P.slots workgroups to fill per K/V head, sum over tiles of their
-// keys / slots, in whole multiples of kMinChunk. One wave, streams over lanes.
+// Chunk length, in whole multiples of kMinChunk: the tiles' keys over the P.slots
+// workgroups there are to fill. Large tiles run in rounds of as many workgroups as are
+// resident, so theirs grows until the chunks fit the rounds (a few left over would take a
+// round of their own). One wave, streams over lanes.
 __device__ __forceinline__ int chunk_length(const CacheAttnArgs& P, int lane) {
-  if (P.slots <= 0) return INT32_MAX / 2;
+  constexpr int kNever = INT32_MAX / 2;
+  if (P.slots <= 0) return kNever;
   uint64_t total = 0;
   for (int s = lane; s < P.streams; s += kWave) {
     const Stream r = stream_of(P, s);
-    total += (uint64_t)r.tiles * (uint64_t)r.span;
+    total += (uint64_t)r.tiles * (uint64_t)r.mean;
   }
   total = wave_sum_u64(total);
-  const uint64_t keys = (total + P.slots - 1) / (uint64_t)P.slots;
-  const uint64_t c = (keys + kMinChunk - 1) / kMinChunk * kMinChunk;
-  return (int)min(max(c, (uint64_t)kMinChunk), (uint64_t)(INT32_MAX / 2));
+  double units = ceil((double)total * P.inv_slots * (1.0 / kMinChunk));
+  if (!(units < kNever / kMinChunk)) return kNever;
+  int n = max((int)units, 1);
+  for (int tries = 0; P.rows == kBigRows && tries < 12; ++tries) {
+    const int chunk = n * kMinChunk;
+    uint64_t items = 0;
+    for (int s = lane; s < P.streams; s += kWave) {
+      const Stream r = stream_of(P, s);
+      items += (uint64_t)r.tiles * (uint64_t)chunks_of(r.mean, chunk);
+    }
+    if (wave_sum_u64(items) <= (uint64_t)P.slots) break;
+    n = min(n + max(n >> 2, 1), kNever / kMinChunk);
+  }
+  return n * kMinChunk;
 }
 
 __device__ __forceinline__ Split split_of(const CacheAttnArgs& P, int item, int lane) {
@@ -696,62 +712,95 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   }
 }
 
-// One wave per query row: the partial results of its tile's chunks, in chunk order.
+// 16 rows of a tile per workgroup: the partial results of the tile's chunks, in chunk
+// order. A wave takes a row at a time: lane c the reference and sum of chunk c (64 chunks
+// at a time), then the chunks' rows with all loads independent.
 __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = (int)(id / P.heads), h = (int)(id % P.heads);
-  if (n >= P.tokens) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int parts = P.rows / 16;
+  const int part = blockIdx.x % parts;
+  const int kh = blockIdx.x / parts % P.kv_heads;
+  const int tile_id = blockIdx.x / parts / P.kv_heads;
   const int chunk = chunk_length(P, lane);
-  // the stream that holds token row n, and its first item
-  int base = 0, stream = -1, item0 = 0;
+  // the stream that holds tile tile_id, its first tile and its first item
+  int tiles = 0, items = 0, stream = -1, tile = 0, item0 = 0;
   for (int s0 = 0; s0 < P.streams; s0 += kWave) {
     const int s = s0 + lane;
-    int cnt = 0;
-    bool holds = false;
+    int t = 0, n = 0;
     if (s < P.streams) {
       const Stream st = stream_of(P, s);
-      cnt = st.tiles * chunks_of(st.span, chunk);
-      holds = n >= st.q0 && n < st.q0 + st.q_len;
+      t = st.tiles;
+      n = st.tiles * chunks_of(st.span, chunk);
     }
-    const int incl = wave_incl_scan_i32(cnt, lane);
-    const uint64_t at = __ballot(holds);
-    if (at) {
-      const int l = __builtin_ctzll(at);
+    const int it = wave_incl_scan_i32(t, lane), in = wave_incl_scan_i32(n, lane);
+    const uint64_t past = __ballot(tiles + it > tile_id);
+    if (past) {
+      const int l = __builtin_ctzll(past);
       stream = s0 + l;
-      item0 = base + __builtin_amdgcn_readlane(incl - cnt, l);
+      tile = tile_id - tiles - __builtin_amdgcn_readlane(it - t, l);
+      item0 = items + __builtin_amdgcn_readlane(in - n, l);
       break;
     }
-    base += __builtin_amdgcn_readlane(incl, 63);
+    tiles += __builtin_amdgcn_readlane(it, 63);
+    items += __builtin_amdgcn_readlane(in, 63);
   }
   if (stream < 0) return;
   const Stream st = stream_of(P, stream);
-  const int kh = h / P.group;
-  const int row = (n - st.q0) * P.group + h - kh * P.group;
-  const int tile = row >> P.row_shift, r = row & (P.rows - 1);
   const Span span = tile_span(P, st, tile);
   const int n_chunks = max(1, (int)ceil_div(span.end - span.begin, chunk));
   if (n_chunks == 1) return;
   const int64_t first = (int64_t)(item0 + tile * chunks_of(st.span, chunk)) * P.kv_heads + kh;
   if (first + (int64_t)(n_chunks - 1) * P.kv_heads >= P.items) return;  // starts that are not ascending
-  float m = -1.0e30f, sum = 0.f;
-  float2 acc = make_float2(0.f, 0.f);
-  for (int c = 0; c < n_chunks; ++c) {
-    const float* part = P.partial + (first + (int64_t)c * P.kv_heads) * (P.rows * (kHeadDim + 2));
-    const float pm = part[P.rows * kHeadDim + r], pl = part[P.rows * kHeadDim + P.rows + r];
-    const float2 po = *reinterpret_cast<const float2*>(part + r * kHeadDim + 2 * lane);
-    const float to = fmaxf(m, pm);
-    const float a = __builtin_amdgcn_exp2f(m - to), b = __builtin_amdgcn_exp2f(pm - to);
-    acc.x = acc.x * a + po.x * b;
-    acc.y = acc.y * a + po.y * b;
-    sum = sum * a + pl * b;
-    m = to;
+  const int64_t size = P.rows * (kHeadDim + 2);
+  const float* base = P.partial + first * size;
+  const int64_t step = P.kv_heads * size;
+  const int rows = st.q_len * P.group;
+  for (int r = 16 * part + wave; r < 16 * part + 16; r += 4) {
+    const int row = tile * P.rows + r;
+    if (row >= rows) break;
+    float m = -1.0e30f, sum = 0.f;
+    float2 acc = make_float2(0.f, 0.f);
+    for (int c0 = 0; c0 < n_chunks; c0 += kWave) {
+      const int n = min(n_chunks - c0, kWave);
+      const float* at = base + (int64_t)(c0 + min(lane, n - 1)) * step + P.rows * kHeadDim + r;
+      const float pm = at[0], pl = at[P.rows];
+      float to = pm;
+#pragma unroll
+      for (int d = 1; d < kWave; d <<= 1) to = fmaxf(to, __shfl_xor(to, d));
+      to = fmaxf(to, m);
+      const float w = lane < n ? __builtin_amdgcn_exp2f(pm - to) : 0.f;
+      const float keep = __builtin_amdgcn_exp2f(m - to);
+      float add = w * pl;
+#pragma unroll
+      for (int d = 1; d < kWave; d <<= 1) add += __shfl_xor(add, d);
+      sum = sum * keep + add;
+      acc.x *= keep;
+      acc.y *= keep;
+      const float* rowp = base + (int64_t)c0 * step + (int64_t)r * kHeadDim + 2 * lane;
+      for (int c = 0; c < n; c += 8) {
+        float2 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const float2*>(rowp + (int64_t)min(c + i, n - 1) * step);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (c + i < n) {
+            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), c + i));
+            acc.x = fmaf(f, v[i].x, acc.x);
+            acc.y = fmaf(f, v[i].y, acc.y);
+          }
+        }
+      }
+      m = to;
+    }
+    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+    const int tok = row / P.group;
+    const int qh = kh * P.group + row - tok * P.group;
+    bf16x2 v;
+    v[0] = (__bf16)(acc.x * inv);
+    v[1] = (__bf16)(acc.y * inv);
+    *reinterpret_cast<bf16x2*>(static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + tok) * P.stride_n + (int64_t)qh * P.stride_h + 2 * lane) = v;
   }
-  const float inv = sum > 0.f ? 1.0f / sum : 0.f;
-  bf16x2 v;
-  v[0] = (__bf16)(acc.x * inv);
-  v[1] = (__bf16)(acc.y * inv);
-  *reinterpret_cast<bf16x2*>(static_cast<uint16_t*>(P.O) + (int64_t)n * P.stride_n + (int64_t)h * P.stride_h + 2 * lane) = v;
 }
 
 // Which kernel, the workgroups per K/V head to split for (0: the tiles alone fill the
@@ -759,7 +808,7 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
 struct Sizes {
   bool big;
   int rows, slots;
-  int64_t items;
+  int64_t tiles, items;
 };
 Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
   const int group = heads / kv_heads;
@@ -768,17 +817,21 @@ Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int max_q, int6
   // that share the keys' conversion through LDS in large tiles.
   r.big = (int64_t)max_q * group > kRows;
   r.rows = r.big ? kBigRows : kRows;
-  const int64_t tiles = (int64_t)tokens * group / r.rows + streams;  // at most one partly filled tile a stream
-  r.slots = std::max(1, (r.big ? kBigSlots : kCacheSlots) / kv_heads);
-  if (most_keys <= kMinChunk || tiles >= 4 * (int64_t)r.slots) r.slots = 0;
-  r.items = tiles + r.slots;
+  r.tiles = (int64_t)tokens * group / r.rows + streams;  // at most one partly filled tile a stream
+  const int round = std::max(1, (r.big ? kBigSlots : kCacheSlots) / kv_heads);
+  const int64_t full = ((int64_t)tokens * group + r.rows - 1) / r.rows;  // tiles if the rows fill them
+  // From two rounds of tiles on their own, chunks no longer pay for the merge.
+  r.slots = most_keys <= kMinChunk || full >= 2 * (int64_t)round ? 0 : (full > round ? 2 : 1) * round;
+  // chunks_of(span) <= 2 chunks_of(mean), and that sum is at most slots + tiles
+  r.items = r.slots ? 2 * (r.tiles + r.slots) : r.tiles;
   return r;
 }
 
 }  // namespace
 
 int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
-  return sizes_of(tokens, heads, kv_heads, streams, max_q, most_keys).items * kv_heads + kXcds;
+  const Sizes z = sizes_of(tokens, heads, kv_heads, streams, max_q, most_keys);
+  return std::max(z.items, z.tiles * (z.rows / 16)) * kv_heads + kXcds;
 }
 
 size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
@@ -794,12 +847,13 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
   a.rows = z.rows;
   a.row_shift = z.big ? 7 : 4;
   a.slots = z.slots;
+  a.inv_slots = z.slots ? 1.0 / z.slots : 0.0;
   a.items = z.items * a.kv_heads;
   if (z.big)
     cache_attn_big_kernel<<<(unsigned)((a.items + kXcds - 1) / kXcds * kXcds), kWaves * kWave, 0, a.stream>>>(a);
   else
     cache_attn_kernel<<<(unsigned)a.items, kWaves * kWave, 0, a.stream>>>(a);
-  if (z.slots) cache_combine_kernel<<<(unsigned)(((int64_t)a.tokens * a.heads + 3) / 4), 256, 0, a.stream>>>(a);
+  if (z.slots) cache_combine_kernel<<<(unsigned)(z.tiles * a.kv_heads * (z.rows / 16)), 256, 0, a.stream>>>(a);
   return hipGetLastError();
 }
 

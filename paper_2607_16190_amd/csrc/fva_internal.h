@@ -169,7 +169,8 @@ struct CacheAttnArgs {
   int group = 1;       // query heads per K/V head
   int rows = 16, row_shift = 4;  // query rows of a tile, a power of two
   int slots = 0;       // workgroups per K/V head that the keys are split for; 0: not split
-  int64_t items = 0;   // partial results there is room for
+  double inv_slots = 0.0;  // 1 / slots
+  int64_t items = 0;   // items, and partial results, there is room for
 };
 
 hipError_t launch_cache_plan(const PlanArgs& a);

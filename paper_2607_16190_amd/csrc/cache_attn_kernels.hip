@@ -42,7 +42,7 @@ constexpr int kRows = 16;        // query rows of a small tile: one MFMA column 
 constexpr int kBigRows = 128;    // query rows of a large tile: 32 for each wave
 constexpr int kKeys = 64;        // keys a wave takes at a time
 constexpr int kWaves = 4;        // waves of a workgroup, each on every fourth 64 keys
-constexpr int kCacheSlots = 1024; // workgroups to split for, small tiles: four a CU
+constexpr int kCacheSlots = 2048; // workgroups to split for, small tiles
 constexpr int kBigSlots = 512;    // large tiles: two a CU, as many as are resident
 constexpr int kXcds = 8;
 constexpr int kMinChunk = kWaves * kKeys;  // a shorter chunk leaves waves without keys
@@ -70,7 +70,7 @@ __device__ __forceinline__ Stream stream_of(const CacheAttnArgs& P, int s) {
   int64_t span = r.kv_len;
   if (P.window) span = min(span, (int64_t)P.window + 2 * (int64_t)P.frame + P.rows + kKeys);
   r.span = (int)span;
-  r.mean = P.frame ? (int)min(span, max((int64_t)r.kv_len - (r.q_len >> 1), (int64_t)((r.kv_len + 1) >> 1))) : r.span;
+  r.mean = P.ramp ? (int)min(span, max((int64_t)r.kv_len - (r.q_len >> 1), (int64_t)((r.kv_len + 1) >> 1))) : r.span;
   return r;
 }
 
@@ -416,6 +416,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) unsigned char lds_u8;
 typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+typedef __attribute__((address_space(4))) const int32_t const_i32;
 
 template <int B, int E, typename F>
 __device__ __forceinline__ void static_for(F&& f) {
@@ -425,13 +426,24 @@ __device__ __forceinline__ void static_for(F&& f) {
   }
 }
 
+__device__ __forceinline__ bf16x8 to_bf16x8(f32x4 a, f32x4 b) {
+  return __builtin_convertvector(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
+}
+
+// s * c2 + negm, an exponential's argument, in the score's own register (sharing one
+// temporary, each would wait for the exponential before it).
+__device__ __forceinline__ float exp2_arg(float s, float c2, float negm) {
+  asm("v_fma_f32 %0, %1, %0, %2" : "+v"(s) : "s"(c2), "v"(negm));
+  return s;
+}
+
 // A large tile: 128 query rows, 32 per wave, against one chunk of its keys, 64 at a time.
 //
 // The 64 keys' codes are read once for the workgroup (two 16-byte pieces of K and of V per
 // thread, while the 64 before them are multiplied), become bf16 in registers and go to
 // LDS, where all four waves read them: a conversion is paid once for 128 rows. LDS holds
 // two such steps. Rows of 256 bytes; K's 16-byte chunk c of row r lies at c ^ r % 16, V's
-// at c ^ 2 (r % 8): the reads of both products are free of bank conflicts.
+// at c ^ (2 (r % 8) + r % 2): the reads of both products meet no bank twice.
 //
 // Bound by the matrix and vector units together (64 + 4 products of 16 passes a wave and
 // step against 32 exponentials and their arguments, maxima and conversions).
@@ -481,6 +493,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
       const int tok = row / P.group;
       const int qh = kh * P.group + row - tok * P.group;
       visible(P, st, tok, lo[nt], hi[nt]);
+      hi[nt] = max(min(hi[nt], k1), lo[nt]);
       const uint16_t* q = static_cast<const uint16_t*>(P.Q) + (int64_t)(st.q0 + tok) * P.stride_n + (int64_t)qh * P.stride_h;
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) qf[nt][ks] = *reinterpret_cast<const bf16x8*>(q + 32 * ks + 8 * g);
@@ -507,37 +520,57 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   const int32_t* table = P.table + (int64_t)sp.stream * P.width;
   const float c2 = P.scale * 1.44269504088896340736f;
 
-  // This thread's two pieces of a step: rows 8 wave + lane / 8 and 32 more, 16 channels
-  // from 16 (lane % 8) on. The eight rows of a wave lie in one page.
-  const int pr = lane >> 3, pc = lane & 7;
+  // This thread's two pieces of a step: 16 channels from 16 pc on of rows 8 wave + pr and
+  // 32 more. The eight rows of a wave lie in one page. Eight neighbouring lanes take four
+  // pieces of two rows of different parity, so that their writes to LDS meet all banks.
+  const int pr = ((lane >> 2) & 1) | ((lane >> 4) << 1), pc = (lane & 3) | ((lane >> 1) & 4);
   uint4 kraw[2], vraw[2];
   float ke[2], ve[2];
+  // Pages and exponents go through the scalar unit: wave-uniform, and nothing here writes
+  // them. The page of a step is asked for two steps before it is multiplied, its exponents
+  // and codes one step. Keys outside [span.lo, k1) repeat the nearest one inside.
+  const const_i32* tab = (const const_i32*)table;
+  const const_i32* kexp = (const const_i32*)P.k_exp + kh;
+  const const_i32* vexp = (const const_i32*)P.v_exp + kh;
+  auto entry_at = [&](int at) { return tab[min(max(at, span.lo), k1 - 1) >> P.page_shift]; };
+  auto page_of = [&](int entry) { return min(max(entry, 0), P.pages - 1); };
+  int page[2];
   auto fetch = [&](int base) {
+    const bool inside = base >= span.lo && base + kKeys <= k1;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      // keys outside [span.lo, k1) repeat the nearest one inside
       const int at = base + 32 * u + 8 * wave;
-      const int first = min(max(at, span.lo), k1 - 1);
-      const int entry = __builtin_amdgcn_readfirstlane(min(max(table[first >> P.page_shift], 0), P.pages - 1));
-      const int64_t tile_at = (int64_t)entry * P.kv_heads + kh;
-      ke[u] = exp_of(P.k_exp[tile_at]);
-      ve[u] = exp_of(P.v_exp[tile_at]);
-      const int r = min(max(at + pr, span.lo), k1 - 1) & (P.page - 1);
-      const int64_t off = tile_at * (P.page * kHeadDim) + r * kHeadDim + 16 * pc;
-      kraw[u] = *reinterpret_cast<const uint4*>(P.k8 + off);
-      vraw[u] = *reinterpret_cast<const uint4*>(P.v8 + off);
+      const int64_t tile_at = ((int64_t)page[u] * P.kv_heads + kh) * (P.page * kHeadDim);
+      uint32_t off;
+      if (inside)
+        off = (uint32_t)((at & (P.page - 1)) * kHeadDim) + (uint32_t)(pr * kHeadDim + 16 * pc);
+      else
+        off = (uint32_t)((min(max(at + pr, span.lo), k1 - 1) & (P.page - 1)) * kHeadDim + 16 * pc);
+      kraw[u] = *reinterpret_cast<const uint4*>(P.k8 + tile_at + off);
+      vraw[u] = *reinterpret_cast<const uint4*>(P.v8 + tile_at + off);
     }
   };
-  auto stage = [&](int buf) {
-    unsigned char* kt = lds + buf * kTile;
-    unsigned char* vt = lds + (2 + buf) * kTile;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int r = 32 * u + 8 * wave + pr;
-      *reinterpret_cast<bf16x8*>(kt + r * kRow + 16 * ((2 * pc) ^ (r & 15))) = eight_bf16(kraw[u].x, kraw[u].y, ke[u]);
-      *reinterpret_cast<bf16x8*>(kt + r * kRow + 16 * ((2 * pc + 1) ^ (r & 15))) = eight_bf16(kraw[u].z, kraw[u].w, ke[u]);
-      *reinterpret_cast<bf16x8*>(vt + r * kRow + 16 * ((2 * pc) ^ (2 * (r & 7)))) = eight_bf16(vraw[u].x, vraw[u].y, ve[u]);
-      *reinterpret_cast<bf16x8*>(vt + r * kRow + 16 * ((2 * pc + 1) ^ (2 * (r & 7)))) = eight_bf16(vraw[u].z, vraw[u].w, ve[u]);
+  const int kx = pr + 8 * (wave & 1), vx = 2 * pr + (pr & 1);  // swizzles of the thread's rows (32 rows on the same)
+  auto stage_k = [&](int buf, int u) {
+    unsigned char* at = lds + buf * kTile + (32 * u + 8 * wave + pr) * kRow;
+    *reinterpret_cast<bf16x8*>(at + 16 * ((2 * pc) ^ kx)) = eight_bf16(kraw[u].x, kraw[u].y, ke[u]);
+    *reinterpret_cast<bf16x8*>(at + 16 * ((2 * pc + 1) ^ kx)) = eight_bf16(kraw[u].z, kraw[u].w, ke[u]);
+  };
+  auto stage_v = [&](int buf, int u) {
+    unsigned char* at = lds + (2 + buf) * kTile + (32 * u + 8 * wave + pr) * kRow;
+    *reinterpret_cast<bf16x8*>(at + 16 * ((2 * pc) ^ vx)) = eight_bf16(vraw[u].x, vraw[u].y, ve[u]);
+    *reinterpret_cast<bf16x8*>(at + 16 * ((2 * pc + 1) ^ vx)) = eight_bf16(vraw[u].z, vraw[u].w, ve[u]);
+  };
+  // (Opaque: the compiler would move a piece's conversion, which both branches of a step
+  // have, up to its load, and wait for it there.)
+  auto stage = [&](int buf, int piece) {
+    const int u = piece & 1;
+    if (piece < 2) {
+      asm volatile("" : "+v"(kraw[u].x), "+v"(kraw[u].y), "+v"(kraw[u].z), "+v"(kraw[u].w));
+      stage_k(buf, u);
+    } else {
+      asm volatile("" : "+v"(vraw[u].x), "+v"(vraw[u].y), "+v"(vraw[u].z), "+v"(vraw[u].w));
+      stage_v(buf, u);
     }
   };
 
@@ -567,54 +600,62 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
     // transposing reads: lane 4 e + q of group g points at row 16 hf + 4 g + e, 8-byte chunk 4 mt + q
     const int vr = 4 * g + (l >> 2);
 #pragma unroll
-    for (int mt = 0; mt < 8; ++mt) vaddr[mt] = base + 2 * kTile + vr * kRow + 8 * (4 * (mt ^ (vr & 7)) + (l & 3));
+    for (int mt = 0; mt < 8; ++mt) vaddr[mt] = base + 2 * kTile + vr * kRow + 16 * ((2 * mt + ((l >> 1) & 1)) ^ (2 * (vr & 7) + (vr & 1))) + 8 * (l & 1);
   }
 
-  if (k0 < k1) {
-    fetch(k0);
-    stage(0);
-  }
-  __syncthreads();
-  int buf = 0;
-  for (int base = k0; base < k1; base += kKeys) {
-    const bool more = base + kKeys < k1;
-    if (more) fetch(base + kKeys);
-    if (base < wave_hi && base + kKeys > wave_lo) {
-      auto kfrag = [&](int t, int ks) { return *(lds_bf16x8*)((lds_u8*)(uintptr_t)kaddr[ks] + buf * kTile + t * 16 * kRow); };
-      auto vfrag = [&](int kk, int mt) {
-        lds_u8* at = (lds_u8*)(uintptr_t)vaddr[mt] + buf * kTile + kk * 32 * kRow;
-        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * kRow));
-        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-      };
-      // S^T: step u takes key tile 2 (u / 8) + u % 2 at channels 32 (u % 8 / 2): four
+  // One step: S^T, the softmax, O^T += V^T P^T from buffer BUF, and the next step's codes
+  // into the other one. (The two buffers are two copies of the code: their offsets are
+  // immediate.)
+  auto step = [&](auto buf_c, int base) {
+    constexpr int BUF = decltype(buf_c)::value;
+    auto kfrag = [&](int t, int ks) { return *(lds_bf16x8*)((lds_u8*)(uintptr_t)kaddr[ks] + BUF * kTile + t * 16 * kRow); };
+    auto vfrag = [&](int kk, int mt) {
+      lds_u8* at = (lds_u8*)(uintptr_t)vaddr[mt] + BUF * kTile + kk * 32 * kRow;
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * kRow));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const bool act = base < wave_hi && base + kKeys > wave_lo;  // wave-uniform
+    fetch(base + kKeys);  // (behind the last step: the last key again)
+    f32x4 s[4][NT];
+    if (act) {
+      // Step u takes key tile 2 (u / 8) + u % 2 at channels 32 (u % 8 / 2): four
       // independent chains alternate; fragments are read two steps ahead.
-      f32x4 s[4][NT];
-      {
-        bf16x8 kq[3];
-        kq[0] = kfrag(0, 0);
-        kq[1] = kfrag(1, 0);
-        __builtin_amdgcn_s_setprio(2);
-        static_for<0, 16>([&](auto u_c) {
-          constexpr int u = decltype(u_c)::value;
-          constexpr int t = 2 * (u >> 3) + (u & 1), ks = (u & 7) >> 1;
-          if constexpr (u + 2 < 16) kq[(u + 2) % 3] = kfrag(2 * ((u + 2) >> 3) + (u & 1), ((u + 2) & 7) >> 1);
+      bf16x8 kq[3];
+      kq[0] = kfrag(0, 0);
+      kq[1] = kfrag(1, 0);
+      __builtin_amdgcn_s_setprio(2);
+      static_for<0, 16>([&](auto u_c) {
+        constexpr int u = decltype(u_c)::value;
+        constexpr int t = 2 * (u >> 3) + (u & 1), ks = (u & 7) >> 1;
+        if constexpr (u + 2 < 16) kq[(u + 2) % 3] = kfrag(2 * ((u + 2) >> 3) + (u & 1), ((u + 2) & 7) >> 1);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-            s[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kq[u % 3], qf[nt][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t][nt], 0, 0, 0);
-          __builtin_amdgcn_sched_barrier(0);
-        });
-        __builtin_amdgcn_s_setprio(0);
-      }
+        for (int nt = 0; nt < NT; ++nt)
+          s[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kq[u % 3], qf[nt][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t][nt], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      __builtin_amdgcn_s_setprio(0);
+    }
+    int kx_[2], vx_[2], ent[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      kx_[u] = kexp[(int64_t)page[u] * P.kv_heads];
+      vx_[u] = vexp[(int64_t)page[u] * P.kv_heads];
+      ent[u] = entry_at(base + 2 * kKeys + 32 * u + 8 * wave);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8 pb[2][NT];
+    if (act) {
       if (base < all_lo || base + kKeys > all_hi) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int key = base + 16 * t + 4 * g + r;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              if (key < lo[nt] || key >= min(hi[nt], k1)) s[t][nt][r] = -INFINITY;
+            for (int nt = 0; nt < NT; ++nt) {
+              const uint32_t past = (uint32_t)(base + 4 * g - lo[nt]) + (16 * t + r);
+              if (past >= (uint32_t)(hi[nt] - lo[nt])) s[t][nt][r] = -INFINITY;
+            }
           }
         }
       }
@@ -647,43 +688,86 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
           }
         }
       }
-      bf16x8 pb[2][NT];
+      // The exponentials of the first 32 keys; those of the second come under the products
+      // of the first.
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
+      for (int t = 0; t < 2; ++t) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          f32x8 e;
+        for (int r = 0; r < 4; ++r) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(s[2 * kk + (j >> 2)][nt][j & 3], c2, negm[nt]));
-          pb[kk][nt] = __builtin_convertvector(e, bf16x8);
+          for (int nt = 0; nt < NT; ++nt) s[t][nt][r] = __builtin_amdgcn_exp2f(exp2_arg(s[t][nt][r], c2, negm[nt]));
         }
       }
-      // O^T += V^T P^T
-      {
-        bf16x8 vq[3];
-        vq[0] = vfrag(0, 0);
-        vq[1] = vfrag(0, 1);
-        __builtin_amdgcn_s_setprio(1);
-        static_for<0, 16>([&](auto u_c) {
-          constexpr int u = decltype(u_c)::value;
-          constexpr int kk = u >> 3, mt = u & 7;
-          if constexpr (u + 2 < 16) vq[(u + 2) % 3] = vfrag((u + 2) >> 3, (u + 2) & 7);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) pb[0][nt] = to_bf16x8(s[0][nt], s[1][nt]);
+    }
+    // The scalars have come; no LDS read is in flight that this wait would hold up.
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      ke[u] = exp_of(kx_[u]);
+      ve[u] = exp_of(vx_[u]);
+      page[u] = page_of(ent[u]);
+    }
+    if (act) {
+      // O^T += V^T P^T, and the next step's codes to LDS
+      bf16x8 vq[3];
+      vq[0] = vfrag(0, 0);
+      vq[1] = vfrag(0, 1);
+      __builtin_amdgcn_s_setprio(1);
+      static_for<0, 16>([&](auto u_c) {
+        constexpr int u = decltype(u_c)::value;
+        constexpr int kk = u >> 3, mt = u & 7;
+        if constexpr (u + 2 < 16) vq[(u + 2) % 3] = vfrag((u + 2) >> 3, (u + 2) & 7);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          o[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vq[u % 3], pb[kk][nt], o[mt][nt], 0, 0, 0);
+        if constexpr (mt == 7) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
-            o[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vq[u % 3], pb[kk][nt], o[mt][nt], 0, 0, 0);
-          if constexpr (mt == 7) {
+            lsum[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[kk][nt], lsum[nt], 0, 0, 0);
+        }
+        if constexpr (u < 8) {
+          constexpr int t = 2 + (u >> 2), r = u & 3;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              lsum[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[kk][nt], lsum[nt], 0, 0, 0);
+          for (int nt = 0; nt < NT; ++nt) s[t][nt][r] = __builtin_amdgcn_exp2f(exp2_arg(s[t][nt][r], c2, negm[nt]));
+          if constexpr (u == 7) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) pb[1][nt] = to_bf16x8(s[2][nt], s[3][nt]);
           }
-          __builtin_amdgcn_sched_barrier(0);
-        });
-        __builtin_amdgcn_s_setprio(0);
-      }
+        } else if constexpr (u % 2 == 0) {
+          stage(BUF ^ 1, (u - 8) / 2);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      __builtin_amdgcn_s_setprio(0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) stage(BUF ^ 1, i);
     }
-    if (more) stage(buf ^ 1);
     __syncthreads();
-    buf ^= 1;
+  };
+
+  if (k0 < k1) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      page[u] = page_of(entry_at(k0 + 32 * u + 8 * wave));
+      ke[u] = exp_of(kexp[(int64_t)page[u] * P.kv_heads]);
+      ve[u] = exp_of(vexp[(int64_t)page[u] * P.kv_heads]);
+    }
+    fetch(k0);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) page[u] = page_of(entry_at(k0 + kKeys + 32 * u + 8 * wave));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) stage(0, i);
+    __syncthreads();
+    for (int base = k0;;) {
+      step(std::integral_constant<int, 0>{}, base);
+      if ((base += kKeys) >= k1) break;
+      step(std::integral_constant<int, 1>{}, base);
+      if ((base += kKeys) >= k1) break;
+    }
   }
 
   // Accumulator r of (mt, nt): channel 16 mt + 4 g + r of row 16 nt + l.
@@ -822,8 +906,9 @@ Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int max_q, int6
   const int64_t full = ((int64_t)tokens * group + r.rows - 1) / r.rows;  // tiles if the rows fill them
   // From two rounds of tiles on their own, chunks no longer pay for the merge.
   r.slots = most_keys <= kMinChunk || full >= 2 * (int64_t)round ? 0 : (full > round ? 2 : 1) * round;
-  // chunks_of(span) <= 2 chunks_of(mean), and that sum is at most slots + tiles
-  r.items = r.slots ? 2 * (r.tiles + r.slots) : r.tiles;
+  // The sum of chunks_of(mean) is at most slots + tiles, and chunks_of(span) at most twice
+  // that, equal where the mean is the span (always for small tiles).
+  r.items = r.slots ? (r.big ? 2 : 1) * (r.tiles + r.slots) : r.tiles;
   return r;
 }
 
@@ -846,6 +931,7 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
   const Sizes z = sizes_of(a.tokens, a.heads, a.kv_heads, a.streams, a.max_q, (int64_t)a.width * a.page);
   a.rows = z.rows;
   a.row_shift = z.big ? 7 : 4;
+  a.ramp = z.big && a.frame;
   a.slots = z.slots;
   a.inv_slots = z.slots ? 1.0 / z.slots : 0.0;
   a.items = z.items * a.kv_heads;

@@ -170,6 +170,7 @@ struct CacheAttnArgs {
   int rows = 16, row_shift = 4;  // query rows of a tile, a power of two
   int slots = 0;       // workgroups per K/V head that the keys are split for; 0: not split
   double inv_slots = 0.0;  // 1 / slots
+  bool ramp = false;   // rows of a stream see more and more keys: its tiles are weighed by their mean
   int64_t items = 0;   // items, and partial results, there is room for
 };
 

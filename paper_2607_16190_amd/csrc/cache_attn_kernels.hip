@@ -189,9 +189,8 @@ __device__ __forceinline__ bf16x8 eight_bf16(uint32_t lo, uint32_t hi, float sca
   return __builtin_bit_cast(bf16x8, r);
 }
 
-__device__ __forceinline__ float exp_of(int e) {  // 2^e
-  return __uint_as_float((uint32_t)(127 + min(max(e, kCacheExpMin), 120)) << 23);
-}
+// 2^e of a stored exponent, which lies in [kCacheExpMin, 120].
+__device__ __forceinline__ float exp_of(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
 // max over lanes l, l^16, l^32, l^48, and the sum of them.
 __device__ __forceinline__ float max4(float v) {
@@ -447,8 +446,10 @@ __device__ __forceinline__ float exp2_arg(float s, float c2, float negm) {
 //
 // Bound by the matrix and vector units together (64 + 4 products of 16 passes a wave and
 // step against 32 exponentials and their arguments, maxima and conversions).
+template <bool kOnePage>
 __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(CacheAttnArgs P) {
   constexpr int NT = 2;
+  constexpr int NP = kOnePage ? 1 : 2;  // pages of a thread's rows in a step
   constexpr int kRow = 256;
   constexpr int kTile = kKeys * kRow;
   __shared__ __align__(16) unsigned char lds[4 * kTile];  // K, K of the next step, V, V
@@ -525,41 +526,49 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   // pieces of two rows of different parity, so that their writes to LDS meet all banks.
   const int pr = ((lane >> 2) & 1) | ((lane >> 4) << 1), pc = (lane & 3) | ((lane >> 1) & 4);
   uint4 kraw[2], vraw[2];
-  float ke[2], ve[2];
+  float ke[NP], ve[NP];
   // Pages and exponents go through the scalar unit: wave-uniform, and nothing here writes
-  // them. The page of a step is asked for two steps before it is multiplied, its exponents
+  // them (kOnePage: pages of 64 tokens or more, a step lies in one; else a wave's eight rows
+  // do). The page of a step is asked for two steps before it is multiplied, its exponents
   // and codes one step. Keys outside [span.lo, k1) repeat the nearest one inside.
   const const_i32* tab = (const const_i32*)table;
-  const const_i32* kexp = (const const_i32*)P.k_exp + kh;
-  const const_i32* vexp = (const const_i32*)P.v_exp + kh;
+  const const_i32* kexp = (const const_i32*)P.k_exp;
+  const const_i32* vexp = (const const_i32*)P.v_exp;
+  const uint32_t page_bytes = (uint32_t)P.page * kHeadDim;
+  const uint32_t step_pages = (uint32_t)P.kv_heads;
+  // Tile (page, head) of the pool that row `at` lies in, from its block table entry.
   auto entry_at = [&](int at) { return tab[min(max(at, span.lo), k1 - 1) >> P.page_shift]; };
-  auto page_of = [&](int entry) { return min(max(entry, 0), P.pages - 1); };
-  int page[2];
+  auto tile_of = [&](int entry) { return (uint32_t)min(max(entry, 0), P.pages - 1) * step_pages + (uint32_t)kh; };
+  auto row_of = [&](int base, int p) { return base + (kOnePage ? 0 : 32 * p + 8 * wave); };
+  const uint32_t lane_off = (uint32_t)((8 * wave + pr) * kHeadDim + 16 * pc);
+  uint32_t tiles[NP];
   auto fetch = [&](int base) {
     const bool inside = base >= span.lo && base + kKeys <= k1;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int at = base + 32 * u + 8 * wave;
-      const int64_t tile_at = ((int64_t)page[u] * P.kv_heads + kh) * (P.page * kHeadDim);
+      const uint64_t at = (uint64_t)tiles[u % NP] * page_bytes;
       uint32_t off;
       if (inside)
-        off = (uint32_t)((at & (P.page - 1)) * kHeadDim) + (uint32_t)(pr * kHeadDim + 16 * pc);
+        off = (uint32_t)(((kOnePage ? base + 32 * u : (base + 32 * u + 8 * wave)) & (P.page - 1)) * kHeadDim) +
+              (kOnePage ? lane_off : (uint32_t)(pr * kHeadDim + 16 * pc));
       else
-        off = (uint32_t)((min(max(at + pr, span.lo), k1 - 1) & (P.page - 1)) * kHeadDim + 16 * pc);
-      kraw[u] = *reinterpret_cast<const uint4*>(P.k8 + tile_at + off);
-      vraw[u] = *reinterpret_cast<const uint4*>(P.v8 + tile_at + off);
+        off = (uint32_t)((min(max(base + 32 * u + 8 * wave + pr, span.lo), k1 - 1) & (P.page - 1)) * kHeadDim + 16 * pc);
+      kraw[u] = *reinterpret_cast<const uint4*>(P.k8 + at + off);
+      vraw[u] = *reinterpret_cast<const uint4*>(P.v8 + at + off);
     }
   };
   const int kx = pr + 8 * (wave & 1), vx = 2 * pr + (pr & 1);  // swizzles of the thread's rows (32 rows on the same)
-  auto stage_k = [&](int buf, int u) {
-    unsigned char* at = lds + buf * kTile + (32 * u + 8 * wave + pr) * kRow;
-    *reinterpret_cast<bf16x8*>(at + 16 * ((2 * pc) ^ kx)) = eight_bf16(kraw[u].x, kraw[u].y, ke[u]);
-    *reinterpret_cast<bf16x8*>(at + 16 * ((2 * pc + 1) ^ kx)) = eight_bf16(kraw[u].z, kraw[u].w, ke[u]);
-  };
-  auto stage_v = [&](int buf, int u) {
-    unsigned char* at = lds + (2 + buf) * kTile + (32 * u + 8 * wave + pr) * kRow;
-    *reinterpret_cast<bf16x8*>(at + 16 * ((2 * pc) ^ vx)) = eight_bf16(vraw[u].x, vraw[u].y, ve[u]);
-    *reinterpret_cast<bf16x8*>(at + 16 * ((2 * pc + 1) ^ vx)) = eight_bf16(vraw[u].z, vraw[u].w, ve[u]);
+  uint32_t wk[2], wv[2];  // LDS addresses of the two 16-byte halves of a piece
+  {
+    const uint32_t base = (uint32_t)(uintptr_t)(lds_u8*)lds + (uint32_t)((8 * wave + pr) * kRow);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      wk[i] = base + 16 * ((2 * pc + i) ^ kx);
+      wv[i] = base + 2 * kTile + 16 * ((2 * pc + i) ^ vx);
+    }
+  }
+  auto put = [&](uint32_t at, int buf, int u, uint32_t a, uint32_t b, float e) {
+    *(lds_bf16x8*)((lds_u8*)(uintptr_t)at + buf * kTile + 32 * u * kRow) = eight_bf16(a, b, e);
   };
   // (Opaque: the compiler would move a piece's conversion, which both branches of a step
   // have, up to its load, and wait for it there.)
@@ -567,10 +576,12 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
     const int u = piece & 1;
     if (piece < 2) {
       asm volatile("" : "+v"(kraw[u].x), "+v"(kraw[u].y), "+v"(kraw[u].z), "+v"(kraw[u].w));
-      stage_k(buf, u);
+      put(wk[0], buf, u, kraw[u].x, kraw[u].y, ke[u % NP]);
+      put(wk[1], buf, u, kraw[u].z, kraw[u].w, ke[u % NP]);
     } else {
       asm volatile("" : "+v"(vraw[u].x), "+v"(vraw[u].y), "+v"(vraw[u].z), "+v"(vraw[u].w));
-      stage_v(buf, u);
+      put(wv[0], buf, u, vraw[u].x, vraw[u].y, ve[u % NP]);
+      put(wv[1], buf, u, vraw[u].z, vraw[u].w, ve[u % NP]);
     }
   };
 
@@ -602,6 +613,12 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
 #pragma unroll
     for (int mt = 0; mt < 8; ++mt) vaddr[mt] = base + 2 * kTile + vr * kRow + 16 * ((2 * mt + ((l >> 1) & 1)) ^ (2 * (vr & 7) + (vr & 1))) + 8 * (l & 1);
   }
+
+  // (Opaque to the compiler, which would otherwise re-add the lanes' parts at every read.)
+  asm volatile("" : "+v"(vaddr[0]), "+v"(vaddr[1]), "+v"(vaddr[2]), "+v"(vaddr[3]), "+v"(vaddr[4]), "+v"(vaddr[5]),
+               "+v"(vaddr[6]), "+v"(vaddr[7]));
+  asm volatile("" : "+v"(kaddr[0]), "+v"(kaddr[1]), "+v"(kaddr[2]), "+v"(kaddr[3]), "+v"(wk[0]), "+v"(wk[1]), "+v"(wv[0]),
+               "+v"(wv[1]));
 
   // One step: S^T, the softmax, O^T += V^T P^T from buffer BUF, and the next step's codes
   // into the other one. (The two buffers are two copies of the code: their offsets are
@@ -636,12 +653,12 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
       });
       __builtin_amdgcn_s_setprio(0);
     }
-    int kx_[2], vx_[2], ent[2];
+    int k_exp[NP], v_exp[NP], entry[NP];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      kx_[u] = kexp[(int64_t)page[u] * P.kv_heads];
-      vx_[u] = vexp[(int64_t)page[u] * P.kv_heads];
-      ent[u] = entry_at(base + 2 * kKeys + 32 * u + 8 * wave);
+    for (int p = 0; p < NP; ++p) {
+      k_exp[p] = kexp[tiles[p]];
+      v_exp[p] = vexp[tiles[p]];
+      entry[p] = entry_at(row_of(base + 2 * kKeys, p));
     }
     __builtin_amdgcn_sched_barrier(0);
     bf16x8 pb[2][NT];
@@ -705,10 +722,10 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      ke[u] = exp_of(kx_[u]);
-      ve[u] = exp_of(vx_[u]);
-      page[u] = page_of(ent[u]);
+    for (int p = 0; p < NP; ++p) {
+      ke[p] = exp_of(k_exp[p]);
+      ve[p] = exp_of(v_exp[p]);
+      tiles[p] = tile_of(entry[p]);
     }
     if (act) {
       // O^T += V^T P^T, and the next step's codes to LDS
@@ -751,14 +768,14 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
 
   if (k0 < k1) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      page[u] = page_of(entry_at(k0 + 32 * u + 8 * wave));
-      ke[u] = exp_of(kexp[(int64_t)page[u] * P.kv_heads]);
-      ve[u] = exp_of(vexp[(int64_t)page[u] * P.kv_heads]);
+    for (int p = 0; p < NP; ++p) {
+      tiles[p] = tile_of(entry_at(row_of(k0, p)));
+      ke[p] = exp_of(kexp[tiles[p]]);
+      ve[p] = exp_of(vexp[tiles[p]]);
     }
     fetch(k0);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) page[u] = page_of(entry_at(k0 + kKeys + 32 * u + 8 * wave));
+    for (int p = 0; p < NP; ++p) tiles[p] = tile_of(entry_at(row_of(k0 + kKeys, p)));
 #pragma unroll
     for (int i = 0; i < 4; ++i) stage(0, i);
     __syncthreads();
@@ -935,8 +952,11 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
   a.slots = z.slots;
   a.inv_slots = z.slots ? 1.0 / z.slots : 0.0;
   a.items = z.items * a.kv_heads;
-  if (z.big)
-    cache_attn_big_kernel<<<(unsigned)((a.items + kXcds - 1) / kXcds * kXcds), kWaves * kWave, 0, a.stream>>>(a);
+  const unsigned grid = (unsigned)((a.items + kXcds - 1) / kXcds * kXcds);
+  if (z.big && a.page >= kKeys)
+    cache_attn_big_kernel<true><<<grid, kWaves * kWave, 0, a.stream>>>(a);
+  else if (z.big)
+    cache_attn_big_kernel<false><<<grid, kWaves * kWave, 0, a.stream>>>(a);
   else
     cache_attn_kernel<<<(unsigned)a.items, kWaves * kWave, 0, a.stream>>>(a);
   if (z.slots) cache_combine_kernel<<<(unsigned)(z.tiles * a.kv_heads * (z.rows / 16)), 256, 0, a.stream>>>(a);

@@ -424,7 +424,8 @@ fva_status check_cache(const fva_cache* c) {
   if (c->pages <= 0 || c->heads <= 0) return FVA_ERR_SHAPE;
   if (c->head_dim != fva::kHeadDim) return FVA_ERR_UNSUPPORTED;
   if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return FVA_ERR_UNSUPPORTED;
-  if ((int64_t)c->pages * c->page > INT32_MAX) return FVA_ERR_UNSUPPORTED;
+  if ((int64_t)c->pages * c->page > INT32_MAX || (int64_t)c->pages * c->heads >= ((int64_t)1 << 29))
+    return FVA_ERR_UNSUPPORTED;  // 32-bit slots, and byte offsets of the exponents
   if (!aligned16(c->k8) || !aligned16(c->v8) || !aligned4(c->k_exp) || !aligned4(c->v_exp)) return FVA_ERR_INVALID_ARG;
   return FVA_OK;
 }

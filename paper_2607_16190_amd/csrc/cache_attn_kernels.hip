@@ -47,9 +47,6 @@ constexpr int kBigSlots = 512;    // large tiles: two a CU, as many as are resid
 constexpr int kXcds = 8;
 constexpr int kMinChunk = kWaves * kKeys;  // a shorter chunk leaves waves without keys
 
-// Integer division by a positive number, rounded up.
-__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 // One stream's share of the work: its rows, keys and tiles.
 struct Stream {
   int q0, q_len;  // first token row, tokens
@@ -74,80 +71,115 @@ __device__ __forceinline__ Stream stream_of(const CacheAttnArgs& P, int s) {
   return r;
 }
 
-// Which stream an item belongs to, and the chunk length.
-struct Split {
-  int chunk;
-  int stream;  // -1: no such item
-  int item0;   // first item of the stream
+// The keys of a tile, [begin, end) with begin on a multiple of kKeys: those that its first
+// row's window starts with to those that its last row ends with.
+struct Span {
+  int begin, lo, end;
 };
 
 __device__ __forceinline__ int chunks_of(int span, int chunk) { return max(1, (span + chunk - 1) / chunk); }
 
-// Chunk length, in whole multiples of kMinChunk: the tiles' keys over the P.slots
-// workgroups there are to fill. Large tiles run in rounds of as many workgroups as are
-// resident, so theirs grows until the chunks fit the rounds (a few left over would take a
-// round of their own). One wave, streams over lanes.
-__device__ __forceinline__ int chunk_length(const CacheAttnArgs& P, int lane) {
-  constexpr int kNever = INT32_MAX / 2;
-  if (P.slots <= 0) return kNever;
-  uint64_t total = 0;
-  for (int s = lane; s < P.streams; s += kWave) {
-    const Stream r = stream_of(P, s);
-    total += (uint64_t)r.tiles * (uint64_t)r.mean;
-  }
-  total = wave_sum_u64(total);
-  double units = ceil((double)total * P.inv_slots * (1.0 / kMinChunk));
-  if (!(units < kNever / kMinChunk)) return kNever;
-  int n = max((int)units, 1);
-  for (int tries = 0; P.rows == kBigRows && tries < 12; ++tries) {
-    const int chunk = n * kMinChunk;
-    uint64_t items = 0;
-    for (int s = lane; s < P.streams; s += kWave) {
-      const Stream r = stream_of(P, s);
-      items += (uint64_t)r.tiles * (uint64_t)chunks_of(r.mean, chunk);
-    }
-    if (wave_sum_u64(items) <= (uint64_t)P.slots) break;
-    n = min(n + max(n >> 2, 1), kNever / kMinChunk);
-  }
-  return n * kMinChunk;
+// What a wave knows of the whole call: the streams over its lanes, the first 64 of them
+// in registers (the others are looked at again).
+struct Work {
+  Stream mine;
+  int chunk;  // keys of a chunk, in whole multiples of kMinChunk
+  int items;  // per K/V head
+};
+
+template <typename F>
+__device__ __forceinline__ void each_stream(const CacheAttnArgs& P, const Stream& mine, int lane, F&& f) {
+  f(mine);
+  for (int s = lane + kWave; s < P.streams; s += kWave) f(stream_of(P, s));
 }
 
-__device__ __forceinline__ Split split_of(const CacheAttnArgs& P, int item, int lane) {
-  Split r;
-  r.chunk = chunk_length(P, lane);
-  int base = 0;
-  for (int s0 = 0; s0 < P.streams; s0 += kWave) {
-    const int s = s0 + lane;
-    int n = 0;
-    if (s < P.streams) {
-      const Stream st = stream_of(P, s);
-      n = st.tiles * chunks_of(st.span, r.chunk);
+// Chunk length: the tiles' keys over the P.slots workgroups there are to fill. Large tiles
+// run in rounds of as many workgroups as are resident, so theirs grows until the chunks fit
+// the rounds (a few left over would take a round of their own).
+__device__ __forceinline__ Work work_of(const CacheAttnArgs& P, int lane) {
+  constexpr int kNever = INT32_MAX / 2;
+  Work w;
+  w.mine = Stream{0, 0, 0, 0, 0, 0};
+  if (lane < P.streams) w.mine = stream_of(P, lane);
+  w.chunk = kNever;
+  if (P.slots > 0) {
+    uint64_t total = 0;
+    each_stream(P, w.mine, lane, [&](const Stream& r) { total += (uint64_t)r.tiles * (uint64_t)r.mean; });
+    total = wave_sum_u64(total);
+    const double units = ceil((double)total * P.inv_slots * (1.0 / kMinChunk));
+    if (units < kNever / kMinChunk) {
+      int n = max((int)units, 1);
+      for (int tries = 0; P.rows == kBigRows && tries < 12; ++tries) {
+        uint64_t items = 0;
+        each_stream(P, w.mine, lane, [&](const Stream& r) { items += (uint64_t)r.tiles * (uint64_t)chunks_of(r.mean, n * kMinChunk); });
+        if (wave_sum_u64(items) <= (uint64_t)P.slots) break;
+        n = min(n + max(n >> 2, 1), kNever / kMinChunk);
+      }
+      w.chunk = n * kMinChunk;
     }
-    const int incl = wave_incl_scan_i32(n, lane);
-    const uint64_t past = __ballot(base + incl > item);
+  }
+  return w;
+}
+
+// All items, per K/V head (starts that are not ascending could ask for more than there is
+// room for).
+__device__ __forceinline__ int items_of(const CacheAttnArgs& P, const Work& w, int lane) {
+  uint64_t n = 0;
+  each_stream(P, w.mine, lane, [&](const Stream& r) { n += (uint64_t)r.tiles * (uint64_t)chunks_of(r.span, w.chunk); });
+  return (int)min(wave_sum_u64(n), (uint64_t)(P.items / P.kv_heads));
+}
+
+// The stream whose share holds number `at` of the numbers count(stream) of all streams
+// one after the other, -1 for none; `before`: the sum of count before it, `items`: the
+// items before it.
+template <typename F>
+__device__ __forceinline__ int find_share(const CacheAttnArgs& P, const Work& w, int lane, int at, F&& count, int& before, int& items) {
+  before = items = 0;
+  Stream r = w.mine;
+  for (int s0 = 0; s0 < P.streams; s0 += kWave) {
+    if (s0) r = s0 + lane < P.streams ? stream_of(P, s0 + lane) : Stream{0, 0, 0, 0, 0, 0};
+    const int c = count(r), n = r.tiles * chunks_of(r.span, w.chunk);
+    const int ci = wave_incl_scan_i32(c, lane), ni = wave_incl_scan_i32(n, lane);
+    const uint64_t past = __ballot(before + ci > at);
     if (past) {
       const int l = __builtin_ctzll(past);
-      r.stream = s0 + l;
-      r.item0 = base + __builtin_amdgcn_readlane(incl - n, l);
-      return r;
+      before += __builtin_amdgcn_readlane(ci - c, l);
+      items += __builtin_amdgcn_readlane(ni - n, l);
+      return s0 + l;
     }
-    base += __builtin_amdgcn_readlane(incl, 63);
+    before += __builtin_amdgcn_readlane(ci, 63);
+    items += __builtin_amdgcn_readlane(ni, 63);
   }
-  r.stream = -1;
-  r.item0 = base;
-  return r;
+  return -1;
 }
 
-// All items of a call, per K/V head.
-__device__ __forceinline__ int total_items(const CacheAttnArgs& P, int lane) {
-  const int chunk = chunk_length(P, lane);
-  uint64_t n = 0;
-  for (int s = lane; s < P.streams; s += kWave) {
-    const Stream st = stream_of(P, s);
-    n += (uint64_t)st.tiles * (uint64_t)chunks_of(st.span, chunk);
+// A work item: a tile's chunk, keys [k0, k1).
+struct Item {
+  int stream;  // -1: no such item
+  Stream st;
+  int tile, n_chunks, k0, k1;
+  int lo;      // first key that any row sees
+};
+__device__ __forceinline__ Span tile_span(const CacheAttnArgs& P, const Stream& st, int tile);
+__device__ __forceinline__ Item item_of(const CacheAttnArgs& P, const Work& w, int item, int lane) {
+  Item r;
+  int before, items;
+  r.stream = find_share(P, w, lane, item, [&](const Stream& s) { return s.tiles * chunks_of(s.span, w.chunk); }, before, items);
+  if (r.stream < 0) return r;
+  r.st = stream_of(P, r.stream);
+  const int per_tile = chunks_of(r.st.span, w.chunk);
+  r.tile = (item - items) / per_tile;
+  const int chunk = (item - items) - r.tile * per_tile;
+  const Span span = tile_span(P, r.st, r.tile);
+  r.n_chunks = chunks_of(span.end - span.begin, w.chunk);
+  if (chunk >= r.n_chunks) {  // this tile sees fewer keys than the stream's widest
+    r.stream = -1;
+    return r;
   }
-  // (starts that are not ascending could ask for more than there is room for)
-  return (int)min(wave_sum_u64(n), (uint64_t)(P.items / P.kv_heads));
+  r.lo = span.lo;
+  r.k0 = (int)min((int64_t)span.begin + (int64_t)chunk * w.chunk, (int64_t)span.end);
+  r.k1 = (int)min((int64_t)r.k0 + w.chunk, (int64_t)span.end);
+  return r;
 }
 
 // Keys [lo, hi) that token i of a stream sees.
@@ -159,11 +191,6 @@ __device__ __forceinline__ void visible(const CacheAttnArgs& P, const Stream& st
   lo = P.window ? (int)max(end - P.window, (int64_t)0) : 0;
 }
 
-// The keys of a tile, [begin, end) with begin on a multiple of kKeys: those that its first
-// row's window starts with to those that its last row ends with.
-struct Span {
-  int begin, lo, end;
-};
 __device__ __forceinline__ Span tile_span(const CacheAttnArgs& P, const Stream& st, int tile) {
   const int row0 = tile * P.rows;
   const int row1 = min(row0 + P.rows, st.q_len * P.group) - 1;
@@ -224,17 +251,11 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_kernel(CacheAttn
   const int g = lane >> 4, l = lane & 15;
   const int kh = blockIdx.x % P.kv_heads;
   const int item = blockIdx.x / P.kv_heads;
-  const Split sp = split_of(P, item, lane);
-  if (sp.stream < 0) return;
-  const Stream st = stream_of(P, sp.stream);
-  const int per_tile = chunks_of(st.span, sp.chunk);
-  const int tile = (item - sp.item0) / per_tile;
-  const int chunk = (item - sp.item0) - tile * per_tile;
-  const Span span = tile_span(P, st, tile);
-  const int n_chunks = max(1, (int)ceil_div(span.end - span.begin, sp.chunk));
-  if (chunk >= n_chunks) return;
-  const int k0 = (int)min((int64_t)span.begin + (int64_t)chunk * sp.chunk, (int64_t)span.end);
-  const int k1 = (int)min((int64_t)k0 + sp.chunk, (int64_t)span.end);
+  const Work work = work_of(P, lane);
+  const Item it = item_of(P, work, item, lane);
+  if (it.stream < 0) return;
+  const Stream& st = it.st;
+  const int tile = it.tile, n_chunks = it.n_chunks, k0 = it.k0, k1 = it.k1;
 
   // This lane's query row.
   const int row = tile * kRows + l;
@@ -260,7 +281,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_kernel(CacheAttn
   all_lo = __builtin_amdgcn_readfirstlane(all_lo);
   all_hi = __builtin_amdgcn_readfirstlane(all_hi);
 
-  const int32_t* table = P.table + (int64_t)sp.stream * P.width;
+  const int32_t* table = P.table + (int64_t)it.stream * P.width;
   const float c2 = P.scale * 1.44269504088896340736f;
   f32x4 o[8];
 #pragma unroll
@@ -268,26 +289,26 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_kernel(CacheAttn
   float mref = -1.0e30f, lsum = 0.f;
 
   for (int base = k0 + wave * kKeys; base < k1; base += kWaves * kKeys) {
-    // Keys outside [span.lo, k1) repeat the nearest one inside: their pages may be no
+    // Keys outside [lo, k1) repeat the nearest one inside: their pages may be no
     // longer the stream's, and their codes anything.
     uint4 kraw[4][2];
     uint2 vraw[4][4];
     float ke[4], ve[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const int first = min(max(base + 16 * t, span.lo), k1 - 1);
+      const int first = min(max(base + 16 * t, it.lo), k1 - 1);
       const int entry = __builtin_amdgcn_readfirstlane(min(max(table[first >> P.page_shift], 0), P.pages - 1));
       const int64_t at = (int64_t)entry * P.kv_heads + kh;
       ke[t] = exp_of(P.k_exp[at]);
       ve[t] = exp_of(P.v_exp[at]);
       const uint8_t* kp = P.k8 + at * P.page * kHeadDim;
       const uint8_t* vp = P.v8 + at * P.page * kHeadDim;
-      const int kr = min(max(base + 16 * t + l, span.lo), k1 - 1) & (P.page - 1);
+      const int kr = min(max(base + 16 * t + l, it.lo), k1 - 1) & (P.page - 1);
       kraw[t][0] = *reinterpret_cast<const uint4*>(kp + kr * kHeadDim + 16 * g);
       kraw[t][1] = *reinterpret_cast<const uint4*>(kp + kr * kHeadDim + 64 + 16 * g);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int vr = min(max(base + 16 * t + 4 * g + r, span.lo), k1 - 1) & (P.page - 1);
+        const int vr = min(max(base + 16 * t + 4 * g + r, it.lo), k1 - 1) & (P.page - 1);
         vraw[t][r] = *reinterpret_cast<const uint2*>(vp + vr * kHeadDim + 8 * l);
       }
     }
@@ -460,24 +481,18 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   // Work items head by head, the runs of consecutive ones on one XCD (workgroups go to the
   // XCDs in turn): the tiles of a head read its keys out of one L2. Later tiles first: with
   // causal frames they see the most keys.
-  const int total = total_items(P, lane);
+  const Work work = work_of(P, lane);
+  const int total = items_of(P, work, lane);
   const int64_t all = (int64_t)total * P.kv_heads;
   const int64_t run = (all + kXcds - 1) / kXcds;
   const int64_t index = (blockIdx.x % kXcds) * run + blockIdx.x / kXcds;
   if (blockIdx.x / kXcds >= run || index >= all) return;
-  const int kh = (int)(index / total);
+  const int kh = (int)((uint32_t)index / (uint32_t)total);
   const int item = total - 1 - (int)(index - (int64_t)kh * total);
-  const Split sp = split_of(P, item, lane);
-  if (sp.stream < 0) return;
-  const Stream st = stream_of(P, sp.stream);
-  const int per_tile = chunks_of(st.span, sp.chunk);
-  const int tile = (item - sp.item0) / per_tile;
-  const int chunk = (item - sp.item0) - tile * per_tile;
-  const Span span = tile_span(P, st, tile);
-  const int n_chunks = max(1, (int)ceil_div(span.end - span.begin, sp.chunk));
-  if (chunk >= n_chunks) return;
-  const int k0 = (int)min((int64_t)span.begin + (int64_t)chunk * sp.chunk, (int64_t)span.end);
-  const int k1 = (int)min((int64_t)k0 + sp.chunk, (int64_t)span.end);
+  const Item it = item_of(P, work, item, lane);
+  if (it.stream < 0) return;
+  const Stream& st = it.st;
+  const int tile = it.tile, n_chunks = it.n_chunks, k0 = it.k0, k1 = it.k1;
 
   const int rows = st.q_len * P.group;
   const int row0 = tile * kBigRows + 32 * wave;
@@ -518,7 +533,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   wave_lo = __builtin_amdgcn_readfirstlane(wave_lo);
   wave_hi = min(__builtin_amdgcn_readfirstlane(wave_hi), k1);
 
-  const int32_t* table = P.table + (int64_t)sp.stream * P.width;
+  const int32_t* table = P.table + (int64_t)it.stream * P.width;
   const float c2 = P.scale * 1.44269504088896340736f;
 
   // This thread's two pieces of a step: 16 channels from 16 pc on of rows 8 wave + pr and
@@ -530,20 +545,20 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   // Pages and exponents go through the scalar unit: wave-uniform, and nothing here writes
   // them (kOnePage: pages of 64 tokens or more, a step lies in one; else a wave's eight rows
   // do). The page of a step is asked for two steps before it is multiplied, its exponents
-  // and codes one step. Keys outside [span.lo, k1) repeat the nearest one inside.
+  // and codes one step. Keys outside [lo, k1) repeat the nearest one inside.
   const const_i32* tab = (const const_i32*)table;
   const const_i32* kexp = (const const_i32*)P.k_exp;
   const const_i32* vexp = (const const_i32*)P.v_exp;
   const uint32_t page_bytes = (uint32_t)P.page * kHeadDim;
   const uint32_t step_pages = (uint32_t)P.kv_heads;
   // Tile (page, head) of the pool that row `at` lies in, from its block table entry.
-  auto entry_at = [&](int at) { return tab[min(max(at, span.lo), k1 - 1) >> P.page_shift]; };
+  auto entry_at = [&](int at) { return tab[min(max(at, it.lo), k1 - 1) >> P.page_shift]; };
   auto tile_of = [&](int entry) { return (uint32_t)min(max(entry, 0), P.pages - 1) * step_pages + (uint32_t)kh; };
   auto row_of = [&](int base, int p) { return base + (kOnePage ? 0 : 32 * p + 8 * wave); };
   const uint32_t lane_off = (uint32_t)((8 * wave + pr) * kHeadDim + 16 * pc);
   uint32_t tiles[NP];
   auto fetch = [&](int base) {
-    const bool inside = base >= span.lo && base + kKeys <= k1;
+    const bool inside = base >= it.lo && base + kKeys <= k1;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const uint64_t at = (uint64_t)tiles[u % NP] * page_bytes;
@@ -552,7 +567,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
         off = (uint32_t)(((kOnePage ? base + 32 * u : (base + 32 * u + 8 * wave)) & (P.page - 1)) * kHeadDim) +
               (kOnePage ? lane_off : (uint32_t)(pr * kHeadDim + 16 * pc));
       else
-        off = (uint32_t)((min(max(base + 32 * u + 8 * wave + pr, span.lo), k1 - 1) & (P.page - 1)) * kHeadDim + 16 * pc);
+        off = (uint32_t)((min(max(base + 32 * u + 8 * wave + pr, it.lo), k1 - 1) & (P.page - 1)) * kHeadDim + 16 * pc);
       kraw[u] = *reinterpret_cast<const uint4*>(P.k8 + at + off);
       vraw[u] = *reinterpret_cast<const uint4*>(P.v8 + at + off);
     }
@@ -823,33 +838,15 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   const int part = blockIdx.x % parts;
   const int kh = blockIdx.x / parts % P.kv_heads;
   const int tile_id = blockIdx.x / parts / P.kv_heads;
-  const int chunk = chunk_length(P, lane);
-  // the stream that holds tile tile_id, its first tile and its first item
-  int tiles = 0, items = 0, stream = -1, tile = 0, item0 = 0;
-  for (int s0 = 0; s0 < P.streams; s0 += kWave) {
-    const int s = s0 + lane;
-    int t = 0, n = 0;
-    if (s < P.streams) {
-      const Stream st = stream_of(P, s);
-      t = st.tiles;
-      n = st.tiles * chunks_of(st.span, chunk);
-    }
-    const int it = wave_incl_scan_i32(t, lane), in = wave_incl_scan_i32(n, lane);
-    const uint64_t past = __ballot(tiles + it > tile_id);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      stream = s0 + l;
-      tile = tile_id - tiles - __builtin_amdgcn_readlane(it - t, l);
-      item0 = items + __builtin_amdgcn_readlane(in - n, l);
-      break;
-    }
-    tiles += __builtin_amdgcn_readlane(it, 63);
-    items += __builtin_amdgcn_readlane(in, 63);
-  }
+  const Work work = work_of(P, lane);
+  const int chunk = work.chunk;
+  int before, item0;
+  const int stream = find_share(P, work, lane, tile_id, [](const Stream& s) { return s.tiles; }, before, item0);
   if (stream < 0) return;
+  const int tile = tile_id - before;
   const Stream st = stream_of(P, stream);
   const Span span = tile_span(P, st, tile);
-  const int n_chunks = max(1, (int)ceil_div(span.end - span.begin, chunk));
+  const int n_chunks = chunks_of(span.end - span.begin, chunk);
   if (n_chunks == 1) return;
   const int64_t first = (int64_t)(item0 + tile * chunks_of(st.span, chunk)) * P.kv_heads + kh;
   if (first + (int64_t)(n_chunks - 1) * P.kv_heads >= P.items) return;  // starts that are not ascending

@@ -512,16 +512,27 @@ _DTYPES = {torch.bfloat16: FVA_BF16, torch.float16: FVA_FP16, torch.float32: FVA
 
 def _same_device(x, *others):
     """The calls below run on the current device: tensors of another one are refused."""
-    if not x.is_cuda or x.device.index != torch.cuda.current_device():
+    dev = x.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError("tensors must be on the current device")
     for t in others:
-        if t is not None and t.device != x.device:
+        if t is not None and t.get_device() != dev:
             raise ValueError("tensors must be on one device")
 
 
 def _int32(t, what, *shape):
-    if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != shape:
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous int32 tensor of shape {shape}")
+
+
+def _rows_of(x) -> _Desc:
+    """Descriptor of [batch, heads, tokens, head_dim] rows."""
+    if x.dim() != 4:
+        raise ValueError("expected a [batch, heads, tokens, head_dim] tensor")
+    sb, sh, sn, sd = x.stride()
+    if sd != 1:
+        raise ValueError("head_dim must be contiguous")
+    return _Desc(*x.shape, sb, sh, sn)
 
 
 def _empty(make, stream):
@@ -531,6 +542,15 @@ def _empty(make, stream):
         return make()
     with torch.cuda.stream(stream):
         return make()
+
+
+def _like(x, stream):
+    return _empty(lambda: torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device), stream)
+
+
+def _matches(out, x):
+    if out.stride() != x.stride() or out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
+        raise ValueError("out must match its input in shape, strides, dtype and device")
 
 
 def fva_rope(q, k, hw, dims, *, ids=None, origin=(0, 0, 0), theta: float = 10000.0, pairing: int = FVA_ROPE_PAIRS,
@@ -544,31 +564,31 @@ def fva_rope(q, k, hw, dims, *, ids=None, origin=(0, 0, 0), theta: float = 10000
     if q.dtype not in _DTYPES or (k is not None and k.dtype != q.dtype):
         raise ValueError("q and k must share one of bf16, fp16 and fp32")
     _same_device(q, k, ids)
-    xs = (q,) if k is None else (q, k)
     if out is None:
-        out = _empty(lambda: tuple(torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device) for x in xs), stream)
+        q_out, k_out = _like(q, stream), None if k is None else _like(k, stream)
     else:
-        out = (out,) if k is None else tuple(out)
-        for x, y in zip(xs, out):
-            if y.stride() != x.stride() or y.shape != x.shape or y.dtype != x.dtype or y.device != x.device:
-                raise ValueError("out must match its input in shape, strides, dtype and device")
-    qd = _desc_of(q)
-    kd = None if k is None else _desc_of(k)
+        q_out, k_out = (out, None) if k is None else out
+        _matches(q_out, q)
+        if k is not None:
+            _matches(k_out, k)
+    qd, kd = _rows_of(q), None if k is None else _rows_of(k)
     if kd is not None and (kd.batch != qd.batch or kd.tokens != qd.tokens):
         raise ValueError("q and k must share batch and tokens")
     ids_stride = 0
     if ids is not None:
         _int32(ids, "ids", *((qd.tokens,) if ids.dim() == 1 else (qd.batch, qd.tokens)))
         ids_stride = 0 if ids.dim() == 1 else qd.tokens
-    params = _RopeParams(int(hw[0]), int(hw[1]), int(dims[0]), int(dims[1]), int(dims[2]), int(origin[0]),
-                         int(origin[1]), int(origin[2]), int(pairing), int(bool(inverse)), float(theta))
+    rows, cols = hw
+    dim_t, dim_y, dim_x = dims
+    t0, y0, x0 = origin
+    params = _RopeParams(rows, cols, dim_t, dim_y, dim_x, t0, y0, x0, pairing, bool(inverse), theta)
     st = lib.fva_rope(
-        _ptr(q), _ptr(out[0]), ctypes.byref(qd), _ptr(k), None if k is None else _ptr(out[1]),
+        q.data_ptr(), q_out.data_ptr(), ctypes.byref(qd), _ptr(k), _ptr(k_out),
         None if kd is None else ctypes.byref(kd), _DTYPES[q.dtype], ctypes.byref(params), _ptr(ids), ids_stride,
         _stream_ptr(stream),
     )
     _check(st, "fva_rope")
-    return out[0] if k is None else out
+    return q_out if k is None else (q_out, k_out)
 
 
 def fva_cache_plan(held, fresh, state, ring, block_table, page: int, tokens: int, *, out=None, stream=None):
@@ -578,32 +598,40 @@ def fva_cache_plan(held, fresh, state, ring, block_table, page: int, tokens: int
     tokens: rows of the slots and ids. Returns (kv_len, q_start, slots, ids, state).
     """
     _same_device(held, fresh, state, ring, block_table)
-    n = held.shape[0] if held.dim() == 1 else -1
+    n, tokens = held.numel(), int(tokens)
     _int32(held, "held", n)
     _int32(fresh, "fresh", n)
     _int32(state, "state", 3)
     _int32(ring, "ring", ring.numel())
-    _int32(block_table, "block_table", n, block_table.shape[-1])
-    shapes = (n,), (n + 1,), (int(tokens),), (int(tokens),), (3,)
+    width = block_table.shape[-1]
+    _int32(block_table, "block_table", n, width)
+    sizes = [n, n + 1, tokens, tokens, 3]
     if out is None:
-        out = _empty(lambda: tuple(torch.empty(s, dtype=torch.int32, device=held.device) for s in shapes), stream)
+        if tokens < 0:
+            raise ValueError("tokens must not be negative")
+        # one buffer, cut into the five results
+        out = _empty(lambda: torch.empty(sum(sizes), dtype=torch.int32, device=held.device), stream).split_with_sizes(sizes)
     else:
         _same_device(held, *out)
-        for t, s, what in zip(out, shapes, ("kv_len", "q_start", "slots", "ids", "state_out")):
-            _int32(t, what, *s)
+        for t, size, what in zip(out, sizes, ("kv_len", "q_start", "slots", "ids", "state_out")):
+            _int32(t, what, size)
+    kv_len, q_start, slots, ids, state_out = out
     st = lib.fva_cache_plan(
-        _ptr(held), _ptr(fresh), n, int(page), _ptr(state), _ptr(ring), ring.numel(), _ptr(block_table),
-        block_table.shape[1], int(tokens), *map(_ptr, out), _stream_ptr(stream),
+        held.data_ptr(), fresh.data_ptr(), n, page, state.data_ptr(), ring.data_ptr(), ring.numel(),
+        block_table.data_ptr(), width, tokens, kv_len.data_ptr(), q_start.data_ptr(), slots.data_ptr(), ids.data_ptr(),
+        state_out.data_ptr(), _stream_ptr(stream),
     )
     _check(st, "fva_cache_plan")
-    return tuple(out)
+    return kv_len, q_start, slots, ids, state_out
 
 
 def _cache_of(k8, v8, k_exp, v_exp) -> _Cache:
-    for t in (k8, v8):
-        if t.dtype != torch.uint8 or t.dim() != 4 or not t.is_contiguous() or t.shape != k8.shape:
-            raise ValueError("k8 and v8 must be contiguous uint8 tensors [pages, heads, page, 128]")
-    pages, heads, page, d = k8.shape
+    shape = k8.shape
+    if k8.dtype is not torch.uint8 or v8.dtype is not torch.uint8 or len(shape) != 4 or v8.shape != shape:
+        raise ValueError("k8 and v8 must be uint8 tensors [pages, heads, page, 128]")
+    if not k8.is_contiguous() or not v8.is_contiguous():
+        raise ValueError("k8 and v8 must be contiguous")
+    pages, heads, page, d = shape
     _int32(k_exp, "k_exp", pages, heads)
     _int32(v_exp, "v_exp", pages, heads)
     return _Cache(pages, heads, page, d, k8.data_ptr(), v8.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr())
@@ -620,11 +648,12 @@ def fva_cache_store(k, v, slots, k8, v8, k_exp, v_exp, *, stream=None):
     if k.shape != v.shape or k.stride() != v.stride():
         raise ValueError("k and v must share shape and strides")
     _same_device(k, v, slots, k8, v8, k_exp, v_exp)
-    desc = _desc_of(k)
-    if slots.dtype != torch.int32 or not slots.is_contiguous() or slots.numel() != desc.batch * desc.tokens:
+    desc = _rows_of(k)
+    if slots.dtype is not torch.int32 or slots.numel() != desc.batch * desc.tokens or not slots.is_contiguous():
         raise ValueError("slots must be a contiguous int32 tensor with one entry per (batch, token)")
     cache = _cache_of(k8, v8, k_exp, v_exp)
-    st = lib.fva_cache_store(_ptr(k), _ptr(v), ctypes.byref(desc), _ptr(slots), ctypes.byref(cache), _stream_ptr(stream))
+    st = lib.fva_cache_store(k.data_ptr(), v.data_ptr(), ctypes.byref(desc), slots.data_ptr(), ctypes.byref(cache),
+                             _stream_ptr(stream))
     _check(st, "fva_cache_store")
 
 
@@ -648,21 +677,22 @@ def fva_attn_cache(q, k8, v8, k_exp, v_exp, block_table, kv_len, q_start, max_q:
     if q.dtype != torch.bfloat16:
         raise ValueError("q must be bf16")
     _same_device(q, k8, v8, k_exp, v_exp, block_table, kv_len, q_start, out, workspace)
-    desc = _desc_of(q)
+    desc = _rows_of(q)
     cache = _cache_of(k8, v8, k_exp, v_exp)
     n = kv_len.numel()
     _int32(kv_len, "kv_len", n)
     _int32(q_start, "q_start", n + 1)
-    _int32(block_table, "block_table", n, block_table.shape[-1])
+    width = block_table.shape[-1]
+    _int32(block_table, "block_table", n, width)
     if out is None:
-        out = _empty(lambda: torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=q.device), stream)
-    elif out.stride() != q.stride() or out.shape != q.shape or out.dtype != q.dtype:
-        raise ValueError("out must match q in shape, strides and dtype")
-    nbytes = fva_attn_cache_workspace_size(desc, cache, block_table.shape[1], n, max_q)
-    ws = _empty(lambda: _workspace(nbytes, q.device, workspace), stream) if nbytes or workspace is not None else None
+        out = _like(q, stream)
+    else:
+        _matches(out, q)
+    nbytes = fva_attn_cache_workspace_size(desc, cache, width, n, max_q)
+    ws = _empty(lambda: _workspace(nbytes, q.device, workspace), stream) if nbytes else None
     st = lib.fva_attn_cache(
-        _ptr(q), ctypes.byref(desc), ctypes.byref(cache), _ptr(block_table), block_table.shape[1], _ptr(kv_len),
-        _ptr(q_start), n, int(max_q), int(frame), int(window), ctypes.c_float(scale), _ptr(out), _ptr(ws),
+        q.data_ptr(), ctypes.byref(desc), ctypes.byref(cache), block_table.data_ptr(), width, kv_len.data_ptr(),
+        q_start.data_ptr(), n, max_q, frame, window, scale, out.data_ptr(), _ptr(ws),
         0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(stream),
     )
     _check(st, "fva_attn_cache")

@@ -45,6 +45,7 @@ constexpr int kWaves = 4;        // waves of a workgroup, each on every fourth 6
 constexpr int kCacheSlots = 2048; // workgroups to split for, small tiles
 constexpr int kBigSlots = 512;    // large tiles: two a CU, as many as are resident
 constexpr int kXcds = 8;
+constexpr int kFewKeys = 2048;    // streams up to which a small tile's keys stay in one workgroup
 constexpr int kMinChunk = kWaves * kKeys;  // a shorter chunk leaves waves without keys
 
 // One stream's share of the work: its rows, keys and tiles.
@@ -243,9 +244,10 @@ __device__ __forceinline__ float sum4(float v) {
 // of each of the eight rows; a byte permute of two rows' words puts two keys of one
 // channel side by side, as the conversion takes them. Tile m of O^T holds channel 8 l + m,
 // so a lane ends with eight consecutive channels of a query row per accumulator index.
-__global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_kernel(CacheAttnArgs P) {
-  __shared__ __align__(16) float ot[kWaves][kRows][kHeadDim + 4];
-  __shared__ float ms[kWaves][kRows], ls[kWaves][kRows];
+template <int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnArgs P) {
+  __shared__ __align__(16) float ot[WAVES][kRows][kHeadDim + 4];
+  __shared__ float ms[WAVES][kRows], ls[WAVES][kRows];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, l = lane & 15;
@@ -288,7 +290,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_kernel(CacheAttn
   for (int m = 0; m < 8; ++m) o[m] = f32x4{0.f, 0.f, 0.f, 0.f};
   float mref = -1.0e30f, lsum = 0.f;
 
-  for (int base = k0 + wave * kKeys; base < k1; base += kWaves * kKeys) {
+  for (int base = k0 + wave * kKeys; base < k1; base += WAVES * kKeys) {
     // Keys outside [lo, k1) repeat the nearest one inside: their pages may be no
     // longer the stream's, and their codes anything.
     uint4 kraw[4][2];
@@ -401,16 +403,17 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_kernel(CacheAttn
   }
   __syncthreads();
   // Thread: row threadIdx / 16, channels 8 (threadIdx % 16) .. + 7.
+  if (threadIdx.x >= 16 * kRows) return;
   const int orow = threadIdx.x >> 4, oc = 8 * (threadIdx.x & 15);
   const int out_row = tile * kRows + orow;
   if (out_row >= st.q_len * P.group) return;
   float m = ms[0][orow];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) m = fmaxf(m, ms[w][orow]);
+  for (int w = 1; w < WAVES; ++w) m = fmaxf(m, ms[w][orow]);
   float sum = 0.f;
   f32x8 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < WAVES; ++w) {
     const float f = __builtin_amdgcn_exp2f(ms[w][orow] - m);
     sum += f * ls[w][orow];
 #pragma unroll
@@ -828,9 +831,84 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   }
 }
 
-// 16 rows of a tile per workgroup: the partial results of the tile's chunks, in chunk
-// order. A wave takes a row at a time: lane c the reference and sum of chunk c (64 chunks
-// at a time), then the chunks' rows with all loads independent.
+// All-lane reduction by a commutative operation, the same bits in every lane.
+template <typename Op>
+__device__ __forceinline__ float wave_reduce(float v, Op op) {
+  auto with = [&](uint32_t x) { v = op(v, __uint_as_float(x)); };
+  with(dpp_move<0xB1>(__float_as_uint(v)));
+  with(dpp_move<0x4E>(__float_as_uint(v)));
+  with(dpp_move<0x141>(__float_as_uint(v)));
+  with(dpp_move<0x140>(__float_as_uint(v)));
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// ROWS rows of a tile from row r on: the partial results of its chunks in chunk order. Lane
+// c has the reference and sum of chunk c (64 chunks at a time), then the chunks' rows are
+// loaded DEPTH chunks at a time for all ROWS rows, all loads independent; lane i has
+// channels 2 i and 2 i + 1. out(row, value) is called for every row.
+template <int ROWS, int DEPTH, typename F>
+__device__ __forceinline__ void merge_rows(const float* base, int64_t step, int tile_rows, int n_chunks, int r, int lane, F&& out) {
+  float m[ROWS], sum[ROWS];
+  float2 acc[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    m[i] = -1.0e30f;
+    sum[i] = 0.f;
+    acc[i] = make_float2(0.f, 0.f);
+  }
+  for (int c0 = 0; c0 < n_chunks; c0 += kWave) {
+    const int n = min(n_chunks - c0, kWave);
+    const float* at = base + (int64_t)(c0 + min(lane, n - 1)) * step + tile_rows * kHeadDim + r;
+    float w[ROWS], pl[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      w[i] = at[i];
+      pl[i] = at[tile_rows + i];
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const float to = fmaxf(wave_reduce(w[i], [](float a, float b) { return fmaxf(a, b); }), m[i]);
+      const float keep = __builtin_amdgcn_exp2f(m[i] - to);
+      w[i] = lane < n ? __builtin_amdgcn_exp2f(w[i] - to) : 0.f;
+      sum[i] = sum[i] * keep + wave_reduce(w[i] * pl[i], [](float a, float b) { return a + b; });
+      acc[i].x *= keep;
+      acc[i].y *= keep;
+      m[i] = to;
+    }
+    const float* row = base + (int64_t)c0 * step + (int64_t)r * kHeadDim + 2 * lane;
+    for (int c = 0; c < n; c += DEPTH) {
+      float2 v[DEPTH][ROWS];
+#pragma unroll
+      for (int j = 0; j < DEPTH; ++j) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+          v[j][i] = *reinterpret_cast<const float2*>(row + (int64_t)min(c + j, n - 1) * step + i * kHeadDim);
+      }
+#pragma unroll
+      for (int j = 0; j < DEPTH; ++j) {
+        if (c + j < n) {
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) {
+            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w[i]), c + j));
+            acc[i].x = fmaf(f, v[j][i].x, acc[i].x);
+            acc[i].y = fmaf(f, v[j][i].y, acc[i].y);
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    const float inv = sum[i] > 0.f ? 1.0f / sum[i] : 0.f;
+    out(r + i, make_float2(acc[i].x * inv, acc[i].y * inv));
+  }
+}
+
+// 16 rows of a tile per workgroup, four per wave at once; a wave with one row (single
+// tokens: many chunks) takes more of its chunks at once.
 __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -854,51 +932,22 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   const float* base = P.partial + first * size;
   const int64_t step = P.kv_heads * size;
   const int rows = st.q_len * P.group;
-  for (int r = 16 * part + wave; r < 16 * part + 16; r += 4) {
+  auto out = [&](int r, float2 o) {
     const int row = tile * P.rows + r;
-    if (row >= rows) break;
-    float m = -1.0e30f, sum = 0.f;
-    float2 acc = make_float2(0.f, 0.f);
-    for (int c0 = 0; c0 < n_chunks; c0 += kWave) {
-      const int n = min(n_chunks - c0, kWave);
-      const float* at = base + (int64_t)(c0 + min(lane, n - 1)) * step + P.rows * kHeadDim + r;
-      const float pm = at[0], pl = at[P.rows];
-      float to = pm;
-#pragma unroll
-      for (int d = 1; d < kWave; d <<= 1) to = fmaxf(to, __shfl_xor(to, d));
-      to = fmaxf(to, m);
-      const float w = lane < n ? __builtin_amdgcn_exp2f(pm - to) : 0.f;
-      const float keep = __builtin_amdgcn_exp2f(m - to);
-      float add = w * pl;
-#pragma unroll
-      for (int d = 1; d < kWave; d <<= 1) add += __shfl_xor(add, d);
-      sum = sum * keep + add;
-      acc.x *= keep;
-      acc.y *= keep;
-      const float* rowp = base + (int64_t)c0 * step + (int64_t)r * kHeadDim + 2 * lane;
-      for (int c = 0; c < n; c += 8) {
-        float2 v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const float2*>(rowp + (int64_t)min(c + i, n - 1) * step);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (c + i < n) {
-            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), c + i));
-            acc.x = fmaf(f, v[i].x, acc.x);
-            acc.y = fmaf(f, v[i].y, acc.y);
-          }
-        }
-      }
-      m = to;
-    }
-    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+    if (row >= rows) return;
     const int tok = row / P.group;
     const int qh = kh * P.group + row - tok * P.group;
     bf16x2 v;
-    v[0] = (__bf16)(acc.x * inv);
-    v[1] = (__bf16)(acc.y * inv);
+    v[0] = (__bf16)o.x;
+    v[1] = (__bf16)o.y;
     *reinterpret_cast<bf16x2*>(static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + tok) * P.stride_n + (int64_t)qh * P.stride_h + 2 * lane) = v;
-  }
+  };
+  const int r = 16 * part + 4 * wave;
+  const int left = rows - (tile * P.rows + r);
+  if (left > 1)
+    merge_rows<4, 4>(base, step, P.rows, n_chunks, r, lane, out);
+  else if (left == 1)
+    merge_rows<1, 16>(base, step, P.rows, n_chunks, r, lane, out);
 }
 
 // Which kernel, the workgroups per K/V head to split for (0: the tiles alone fill the
@@ -919,7 +968,9 @@ Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int max_q, int6
   const int round = std::max(1, (r.big ? kBigSlots : kCacheSlots) / kv_heads);
   const int64_t full = ((int64_t)tokens * group + r.rows - 1) / r.rows;  // tiles if the rows fill them
   // From two rounds of tiles on their own, chunks no longer pay for the merge.
-  r.slots = most_keys <= kMinChunk || full >= 2 * (int64_t)round ? 0 : (full > round ? 2 : 1) * round;
+  // Nor do they where eight waves go through the keys in four turns of 64 or fewer.
+  const bool few = most_keys <= (r.big ? kMinChunk : kFewKeys);
+  r.slots = few || full >= 2 * (int64_t)round ? 0 : (full > round ? 2 : 1) * round;
   // The sum of chunks_of(mean) is at most slots + tiles, and chunks_of(span) at most twice
   // that, equal where the mean is the span (always for small tiles).
   r.items = r.slots ? (r.big ? 2 : 1) * (r.tiles + r.slots) : r.tiles;
@@ -954,8 +1005,10 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
     cache_attn_big_kernel<true><<<grid, kWaves * kWave, 0, a.stream>>>(a);
   else if (z.big)
     cache_attn_big_kernel<false><<<grid, kWaves * kWave, 0, a.stream>>>(a);
+  else if (!z.slots)
+    cache_attn_kernel<2 * kWaves><<<(unsigned)a.items, 2 * kWaves * kWave, 0, a.stream>>>(a);
   else
-    cache_attn_kernel<<<(unsigned)a.items, kWaves * kWave, 0, a.stream>>>(a);
+    cache_attn_kernel<kWaves><<<(unsigned)a.items, kWaves * kWave, 0, a.stream>>>(a);
   if (z.slots) cache_combine_kernel<<<(unsigned)(z.tiles * a.kv_heads * (z.rows / 16)), 256, 0, a.stream>>>(a);
   return hipGetLastError();
 }

@@ -206,17 +206,19 @@ __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float 
 }
 
 // One wave takes the runs that begin in a window of token rows, for one head and one of
-// K and V. A run is a stretch of rows with consecutive slots in one page. Its rows are
-// read once, into registers (16 lanes a row), their maximum taken, and written as codes.
-// ROWS: the page's tokens.
-template <int ROWS>
+// K and V. A run is a stretch of rows with consecutive slots in one page. Its rows go
+// through registers HOLD at a time (16 lanes a row): a run of up to HOLD rows is read once;
+// of a longer one all but the last HOLD a second time behind the maximum, from the L2.
+// PAGE: the page's tokens.
+template <int PAGE, int HOLD>
 __global__ __launch_bounds__(256) void cache_store_kernel(StoreArgs P) {
-  constexpr int kGroups = ROWS / 4;  // four rows per load
+  constexpr int kGroups = HOLD / 4;  // four rows per load
+  constexpr bool kOnce = PAGE <= HOLD;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
-  const int64_t hv = unit % (2 * P.heads);
-  const int64_t w0 = unit / (2 * P.heads) * P.window;
+  const uint32_t unit = blockIdx.x * 4 + wave;
+  const uint32_t hv = unit % (uint32_t)(2 * P.heads);
+  const int w0 = (int)(unit / (uint32_t)(2 * P.heads)) * P.window;
   const int rows = P.batch * P.tokens;
   if (w0 >= rows) return;
   const int head = (int)(hv >> 1);
@@ -224,81 +226,102 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreArgs P) {
   const uint16_t* src = static_cast<const uint16_t*>(is_v ? P.V : P.K) + (int64_t)head * P.stride_h;
   uint8_t* codes = is_v ? P.v8 : P.k8;
   int32_t* exps = is_v ? P.v_exp : P.k_exp;
-  const int64_t top = (int64_t)P.pages * ROWS;
+  const int top = P.pages * PAGE;
+  const int lr = lane >> 4, lc = lane & 15;
   auto slot_of = [&](int64_t r) { return r >= 0 && r < rows ? P.slots[r] : -1; };
-  const int mine = slot_of(w0 + lane), prev = slot_of(w0 + lane - 1);
-  const bool starts = lane < P.window && mine >= 0 && mine < top && !(prev == mine - 1 && mine % ROWS != 0);
+  const int64_t wr = (int64_t)w0 + lane;
+  const int mine = slot_of(wr), prev = slot_of(wr - 1);
+  const bool starts = lane < P.window && mine >= 0 && mine < top && !(prev == mine - 1 && mine % PAGE != 0);
   for (uint64_t todo = __ballot(starts); todo; todo &= todo - 1) {
     const int at = __builtin_ctzll(todo);
-    const int64_t r0 = w0 + at;
+    const int64_t r0 = (int64_t)w0 + at;
     const int slot = __builtin_amdgcn_readlane(mine, at);
-    const int page = slot / ROWS, off = slot % ROWS;
+    const int page = slot / PAGE, off = slot % PAGE;
     int n;
     {
-      const bool in = off + lane < ROWS && slot_of(r0 + lane) == slot + lane;
+      const bool in = off + lane < PAGE && slot_of(r0 + lane) == slot + lane;
       const uint64_t out = ~__ballot(in);
       n = out ? __builtin_ctzll(out) : 64;
-      if (ROWS > 64 && n == 64) {
-        const bool more = off + 64 + lane < ROWS && slot_of(r0 + 64 + lane) == slot + 64 + lane;
+      if (PAGE > 64 && n == 64) {
+        const bool more = off + 64 + lane < PAGE && slot_of(r0 + 64 + lane) == slot + 64 + lane;
         const uint64_t end = ~__ballot(more);
         n += end ? __builtin_ctzll(end) : 64;
       }
     }
-    const int lr = lane >> 4, lc = lane & 15;
     uint4 x[kGroups];
+    auto load = [&](int row) {  // rows row .. row + HOLD - 1 of the run
 #pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-      x[i] = make_uint4(0, 0, 0, 0);
-      if (4 * i < n) {  // wave-uniform
-        const uint32_t r = (uint32_t)(r0 + min(4 * i + lr, n - 1));
-        const uint32_t b = P.batch == 1 ? 0u : r / (uint32_t)P.tokens;
-        x[i] = *reinterpret_cast<const uint4*>(src + (int64_t)b * P.stride_b + (int64_t)(r - b * (uint32_t)P.tokens) * P.stride_n + 8 * lc);
+      for (int i = 0; i < kGroups; ++i) {
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (row + 4 * i < n) {  // wave-uniform
+          const uint32_t r = (uint32_t)(r0 + min(row + 4 * i + lr, n - 1));
+          const uint32_t b = P.batch == 1 ? 0u : r / (uint32_t)P.tokens;
+          x[i] = *reinterpret_cast<const uint4*>(src + (int64_t)b * P.stride_b + (int64_t)(r - b * (uint32_t)P.tokens) * P.stride_n + 8 * lc);
+        }
+      }
+    };
+    const int64_t tile = (int64_t)page * P.heads + head;
+    const int before = off > 0 ? exps[tile] : kCacheExpMin;
+    float amax = 0.f;
+    for (int row = 0; row < (kOnce ? 1 : n); row += HOLD) {
+      load(row);
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) {
+        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) amax = fmaxf(amax, fmaxf(fabsf(bf16_lo(w[e])), fabsf(bf16_hi(w[e]))));
       }
     }
-    float amax = 0.f;
-#pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) amax = fmaxf(amax, fmaxf(fabsf(bf16_lo(w[e])), fabsf(bf16_hi(w[e]))));
-    }
     int e = cache_exponent(wave_max_abs(amax));
-    const int64_t tile = (int64_t)page * P.heads + head;
-    uint8_t* out = codes + tile * (ROWS * kHeadDim);
-    if (off > 0) {
-      const int before = exps[tile];
-      if (before >= e) {
-        e = before;
-      } else {
-        // the tokens already there, on the new scale: one rounding more
-        const float by = ldexpf(1.f, max(before - e, -60));
-        for (int r = lr; r < off; r += 4) {
-          uint2* p = reinterpret_cast<uint2*>(out + r * kHeadDim + 8 * lc);
-          const uint2 v = *p;
-          float f[8];
+    uint8_t* out = codes + tile * (PAGE * kHeadDim);
+    if (before >= e) {
+      e = before;
+    } else if (off > 0) {
+      // the tokens already there, on the new scale: one rounding more
+      const float by = ldexpf(1.f, max(before - e, -60));
+      for (int r = lr; r < off; r += 4) {
+        uint2* p = reinterpret_cast<uint2*>(out + r * kHeadDim + 8 * lc);
+        const uint2 v = *p;
+        float f[8];
 #pragma unroll
-          for (int d = 0; d < 2; ++d) {
-            const int w = (int)(d ? v.y : v.x);
-            f[4 * d] = __builtin_amdgcn_cvt_f32_fp8(w, 0) * by;
-            f[4 * d + 1] = __builtin_amdgcn_cvt_f32_fp8(w, 1) * by;
-            f[4 * d + 2] = __builtin_amdgcn_cvt_f32_fp8(w, 2) * by;
-            f[4 * d + 3] = __builtin_amdgcn_cvt_f32_fp8(w, 3) * by;
-          }
-          *p = make_uint2(four_codes(f[0], f[1], f[2], f[3]), four_codes(f[4], f[5], f[6], f[7]));
+        for (int d = 0; d < 2; ++d) {
+          const int w = (int)(d ? v.y : v.x);
+          f[4 * d] = __builtin_amdgcn_cvt_f32_fp8(w, 0) * by;
+          f[4 * d + 1] = __builtin_amdgcn_cvt_f32_fp8(w, 1) * by;
+          f[4 * d + 2] = __builtin_amdgcn_cvt_f32_fp8(w, 2) * by;
+          f[4 * d + 3] = __builtin_amdgcn_cvt_f32_fp8(w, 3) * by;
         }
+        *p = make_uint2(four_codes(f[0], f[1], f[2], f[3]), four_codes(f[4], f[5], f[6], f[7]));
       }
     }
     const float inv = __uint_as_float((uint32_t)(127 - min(max(e, kCacheExpMin), 120)) << 23);
+    // the rows that are still held first, the ones before them once more
+    const int last = kOnce ? 0 : (n - 1) / HOLD * HOLD;
+    for (int row = last; row >= 0; row -= HOLD) {
+      if (!kOnce && row < last) load(row);
 #pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-      if (4 * i + lr < n) {
-        const uint2 c = make_uint2(
-            four_codes(bf16_lo(x[i].x) * inv, bf16_hi(x[i].x) * inv, bf16_lo(x[i].y) * inv, bf16_hi(x[i].y) * inv),
-            four_codes(bf16_lo(x[i].z) * inv, bf16_hi(x[i].z) * inv, bf16_lo(x[i].w) * inv, bf16_hi(x[i].w) * inv));
-        *reinterpret_cast<uint2*>(out + (off + 4 * i + lr) * kHeadDim + 8 * lc) = c;
+      for (int i = 0; i < kGroups; ++i) {
+        const int r = row + 4 * i + lr;
+        if (r < n) {
+          const uint2 c = make_uint2(
+              four_codes(bf16_lo(x[i].x) * inv, bf16_hi(x[i].x) * inv, bf16_lo(x[i].y) * inv, bf16_hi(x[i].y) * inv),
+              four_codes(bf16_lo(x[i].z) * inv, bf16_hi(x[i].z) * inv, bf16_lo(x[i].w) * inv, bf16_hi(x[i].w) * inv));
+          *reinterpret_cast<uint2*>(out + (off + r) * kHeadDim + 8 * lc) = c;
+        }
       }
+      if (kOnce) break;
     }
     if (lane == 0) exps[tile] = e;
+  }
+}
+
+template <int HOLD>
+void launch_store(const StoreArgs& a, dim3 grid) {
+  switch (a.page) {
+    case 16: cache_store_kernel<16, 16><<<grid, 256, 0, a.stream>>>(a); break;
+    case 32: cache_store_kernel<32, HOLD < 32 ? HOLD : 32><<<grid, 256, 0, a.stream>>>(a); break;
+    case 64: cache_store_kernel<64, HOLD><<<grid, 256, 0, a.stream>>>(a); break;
+    default: cache_store_kernel<128, HOLD == 64 ? 128 : HOLD><<<grid, 256, 0, a.stream>>>(a); break;
   }
 }
 
@@ -323,12 +346,16 @@ hipError_t launch_cache_store(StoreArgs a) {
   while (a.window > 1 && (rows + a.window - 1) / a.window * 2 * a.heads < 4096) a.window >>= 1;
   const int64_t units = (rows + a.window - 1) / a.window * 2 * a.heads;
   const dim3 grid((unsigned)((units + 3) / 4));
-  switch (a.page) {
-    case 16: cache_store_kernel<16><<<grid, 256, 0, a.stream>>>(a); break;
-    case 32: cache_store_kernel<32><<<grid, 256, 0, a.stream>>>(a); break;
-    case 64: cache_store_kernel<64><<<grid, 256, 0, a.stream>>>(a); break;
-    default: cache_store_kernel<128><<<grid, 256, 0, a.stream>>>(a); break;
-  }
+  // Rows held: small windows go with calls of many single tokens, whose waves should all be
+  // resident (16 rows: eight waves a SIMD); where windows hold whole runs, reading a run
+  // once counts (the page: two waves, one with 128). 3042 rows of 40 heads in pages of
+  // 64 / 128: 20.2 / 29.9 us held whole, 29.2 in 16 rows / 34.5 in 64; 256 single tokens of
+  // 40 heads: 11.2 with 16 rows held, 14.9 with 32, 26.6 with 64; 3042 rows of 5 heads
+  // (short windows, whole runs): 12.3, 10.3, 9.9.
+  if (a.window < 16)
+    launch_store<16>(a, grid);
+  else
+    launch_store<64>(a, grid);
   return hipGetLastError();
 }
 

@@ -84,8 +84,7 @@ __device__ __forceinline__ int chunks_of(int span, int chunk) { return max(1, (s
 // in registers (the others are looked at again).
 struct Work {
   Stream mine;
-  int chunk;  // keys of a chunk, in whole multiples of kMinChunk
-  int items;  // per K/V head
+  int chunk;  // keys of a chunk, at most
 };
 
 template <typename F>
@@ -94,9 +93,10 @@ __device__ __forceinline__ void each_stream(const CacheAttnArgs& P, const Stream
   for (int s = lane + kWave; s < P.streams; s += kWave) f(stream_of(P, s));
 }
 
-// Chunk length: the tiles' keys over the P.slots workgroups there are to fill. Large tiles
+// Longest chunk: the tiles' keys over the P.slots workgroups there are to fill. Large tiles
 // run in rounds of as many workgroups as are resident, so theirs grows until the chunks fit
-// the rounds (a few left over would take a round of their own).
+// the rounds (a few left over would take a round of their own). A stream's keys are then
+// cut into equal chunks of at most that (chunk_of).
 __device__ __forceinline__ Work work_of(const CacheAttnArgs& P, int lane) {
   constexpr int kNever = INT32_MAX / 2;
   Work w;
@@ -107,19 +107,29 @@ __device__ __forceinline__ Work work_of(const CacheAttnArgs& P, int lane) {
     uint64_t total = 0;
     each_stream(P, w.mine, lane, [&](const Stream& r) { total += (uint64_t)r.tiles * (uint64_t)r.mean; });
     total = wave_sum_u64(total);
-    const double units = ceil((double)total * P.inv_slots * (1.0 / kMinChunk));
-    if (units < kNever / kMinChunk) {
-      int n = max((int)units, 1);
-      for (int tries = 0; P.rows == kBigRows && tries < 12; ++tries) {
+    const double units = ceil((double)total * P.inv_slots * (1.0 / kKeys));
+    if (units < kNever / kKeys / 8) {
+      int n = max((int)units, kMinChunk / kKeys);
+      for (int tries = 0; P.rows == kBigRows && tries < 10; ++tries) {
         uint64_t items = 0;
-        each_stream(P, w.mine, lane, [&](const Stream& r) { items += (uint64_t)r.tiles * (uint64_t)chunks_of(r.mean, n * kMinChunk); });
+        each_stream(P, w.mine, lane, [&](const Stream& r) { items += (uint64_t)r.tiles * (uint64_t)chunks_of(r.mean, n * kKeys); });
         if (wave_sum_u64(items) <= (uint64_t)P.slots) break;
-        n = min(n + max(n >> 2, 1), kNever / kMinChunk);
+        n += max(n >> 3, 1);
       }
-      w.chunk = n * kMinChunk;
+      w.chunk = n * kKeys;
     }
   }
   return w;
+}
+
+// A stream's chunk: as many as w.chunk asks for, of equal length in whole steps of the
+// workgroup's waves (fewer where the steps are long: chunks_of(span, chunk_of) is at most
+// chunks_of(span, w.chunk)).
+__device__ __forceinline__ int chunk_of(const CacheAttnArgs& P, const Stream& r, int chunk) {
+  const int n = chunks_of(r.span, chunk);
+  if (n == 1) return chunk;
+  const int unit = P.rows == kBigRows ? kKeys : kMinChunk;
+  return ((r.span + n - 1) / n + unit - 1) / unit * unit;
 }
 
 // All items, per K/V head (starts that are not ascending could ask for more than there is
@@ -132,9 +142,9 @@ __device__ __forceinline__ int items_of(const CacheAttnArgs& P, const Work& w, i
 
 // The stream whose share holds number `at` of the numbers count(stream) of all streams
 // one after the other, -1 for none; `before`: the sum of count before it, `items`: the
-// items before it.
+// items before it, `st`: the stream.
 template <typename F>
-__device__ __forceinline__ int find_share(const CacheAttnArgs& P, const Work& w, int lane, int at, F&& count, int& before, int& items) {
+__device__ __forceinline__ int find_share(const CacheAttnArgs& P, const Work& w, int lane, int at, F&& count, int& before, int& items, Stream& st) {
   before = items = 0;
   Stream r = w.mine;
   for (int s0 = 0; s0 < P.streams; s0 += kWave) {
@@ -146,6 +156,9 @@ __device__ __forceinline__ int find_share(const CacheAttnArgs& P, const Work& w,
       const int l = __builtin_ctzll(past);
       before += __builtin_amdgcn_readlane(ci - c, l);
       items += __builtin_amdgcn_readlane(ni - n, l);
+      st = Stream{__builtin_amdgcn_readlane(r.q0, l), __builtin_amdgcn_readlane(r.q_len, l),
+                  __builtin_amdgcn_readlane(r.kv_len, l), __builtin_amdgcn_readlane(r.tiles, l),
+                  __builtin_amdgcn_readlane(r.span, l), __builtin_amdgcn_readlane(r.mean, l)};
       return s0 + l;
     }
     before += __builtin_amdgcn_readlane(ci, 63);
@@ -165,21 +178,21 @@ __device__ __forceinline__ Span tile_span(const CacheAttnArgs& P, const Stream& 
 __device__ __forceinline__ Item item_of(const CacheAttnArgs& P, const Work& w, int item, int lane) {
   Item r;
   int before, items;
-  r.stream = find_share(P, w, lane, item, [&](const Stream& s) { return s.tiles * chunks_of(s.span, w.chunk); }, before, items);
+  r.stream = find_share(P, w, lane, item, [&](const Stream& s) { return s.tiles * chunks_of(s.span, w.chunk); }, before, items, r.st);
   if (r.stream < 0) return r;
-  r.st = stream_of(P, r.stream);
+  const int keys = chunk_of(P, r.st, w.chunk);
   const int per_tile = chunks_of(r.st.span, w.chunk);
   r.tile = (item - items) / per_tile;
   const int chunk = (item - items) - r.tile * per_tile;
   const Span span = tile_span(P, r.st, r.tile);
-  r.n_chunks = chunks_of(span.end - span.begin, w.chunk);
+  r.n_chunks = chunks_of(span.end - span.begin, keys);
   if (chunk >= r.n_chunks) {  // this tile sees fewer keys than the stream's widest
     r.stream = -1;
     return r;
   }
   r.lo = span.lo;
-  r.k0 = (int)min((int64_t)span.begin + (int64_t)chunk * w.chunk, (int64_t)span.end);
-  r.k1 = (int)min((int64_t)r.k0 + w.chunk, (int64_t)span.end);
+  r.k0 = (int)min((int64_t)span.begin + (int64_t)chunk * keys, (int64_t)span.end);
+  r.k1 = (int)min((int64_t)r.k0 + keys, (int64_t)span.end);
   return r;
 }
 
@@ -917,16 +930,15 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   const int kh = blockIdx.x / parts % P.kv_heads;
   const int tile_id = blockIdx.x / parts / P.kv_heads;
   const Work work = work_of(P, lane);
-  const int chunk = work.chunk;
   int before, item0;
-  const int stream = find_share(P, work, lane, tile_id, [](const Stream& s) { return s.tiles; }, before, item0);
+  Stream st;
+  const int stream = find_share(P, work, lane, tile_id, [](const Stream& s) { return s.tiles; }, before, item0, st);
   if (stream < 0) return;
   const int tile = tile_id - before;
-  const Stream st = stream_of(P, stream);
   const Span span = tile_span(P, st, tile);
-  const int n_chunks = chunks_of(span.end - span.begin, chunk);
+  const int n_chunks = chunks_of(span.end - span.begin, chunk_of(P, st, work.chunk));
   if (n_chunks == 1) return;
-  const int64_t first = (int64_t)(item0 + tile * chunks_of(st.span, chunk)) * P.kv_heads + kh;
+  const int64_t first = (int64_t)(item0 + tile * chunks_of(st.span, work.chunk)) * P.kv_heads + kh;
   if (first + (int64_t)(n_chunks - 1) * P.kv_heads >= P.items) return;  // starts that are not ascending
   const int64_t size = P.rows * (kHeadDim + 2);
   const float* base = P.partial + first * size;

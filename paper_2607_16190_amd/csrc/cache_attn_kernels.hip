@@ -560,8 +560,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   float ke[NP], ve[NP];
   // Pages and exponents go through the scalar unit: wave-uniform, and nothing here writes
   // them (kOnePage: pages of 64 tokens or more, a step lies in one; else a wave's eight rows
-  // do). The page of a step is asked for two steps before it is multiplied, its exponents
-  // and codes one step. Keys outside [lo, k1) repeat the nearest one inside.
+  // do). The page of a step is asked for three steps before it is multiplied, its exponents
+  // and codes two steps. Keys outside [lo, k1) repeat the nearest one inside.
   const const_i32* tab = (const const_i32*)table;
   const const_i32* kexp = (const const_i32*)P.k_exp;
   const const_i32* vexp = (const const_i32*)P.v_exp;
@@ -651,8 +651,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   asm volatile("" : "+v"(kaddr[0]), "+v"(kaddr[1]), "+v"(kaddr[2]), "+v"(kaddr[3]), "+v"(wk[0]), "+v"(wk[1]), "+v"(wv[0]),
                "+v"(wv[1]));
 
-  // One step: S^T, the softmax, O^T += V^T P^T from buffer BUF, and the next step's codes
-  // into the other one. (The two buffers are two copies of the code: their offsets are
+  // One step: S^T, under it the next step's codes into the other buffer and the loads of the
+  // step after that, the softmax, O^T += V^T P^T. (The two buffers are two copies of the code: their offsets are
   // immediate.)
   auto step = [&](auto buf_c, int base) {
     constexpr int BUF = decltype(buf_c)::value;
@@ -664,7 +664,6 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     };
     const bool act = base < wave_hi && base + kKeys > wave_lo;  // wave-uniform
-    fetch(base + kKeys);  // (behind the last step: the last key again)
     f32x4 s[4][NT];
     if (act) {
       // Step u takes key tile 2 (u / 8) + u % 2 at channels 32 (u % 8 / 2): four
@@ -680,16 +679,21 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
           s[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kq[u % 3], qf[nt][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t][nt], 0, 0, 0);
+        if constexpr (u % 4 == 1) stage(BUF ^ 1, u / 4);
         __builtin_amdgcn_sched_barrier(0);
       });
       __builtin_amdgcn_s_setprio(0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) stage(BUF ^ 1, i);
     }
+    fetch(base + 2 * kKeys);  // (behind the last step: the last key again)
     int k_exp[NP], v_exp[NP], entry[NP];
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       k_exp[p] = kexp[tiles[p]];
       v_exp[p] = vexp[tiles[p]];
-      entry[p] = entry_at(row_of(base + 2 * kKeys, p));
+      entry[p] = entry_at(row_of(base + 3 * kKeys, p));
     }
     __builtin_amdgcn_sched_barrier(0);
     bf16x8 pb[2][NT];
@@ -759,7 +763,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
       tiles[p] = tile_of(entry[p]);
     }
     if (act) {
-      // O^T += V^T P^T, and the next step's codes to LDS
+      // O^T += V^T P^T
       bf16x8 vq[3];
       vq[0] = vfrag(0, 0);
       vq[1] = vfrag(0, 1);
@@ -784,31 +788,31 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) pb[1][nt] = to_bf16x8(s[2][nt], s[3][nt]);
           }
-        } else if constexpr (u % 2 == 0) {
-          stage(BUF ^ 1, (u - 8) / 2);
         }
         __builtin_amdgcn_sched_barrier(0);
       });
       __builtin_amdgcn_s_setprio(0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) stage(BUF ^ 1, i);
     }
     __syncthreads();
   };
 
   if (k0 < k1) {
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      tiles[p] = tile_of(entry_at(row_of(k0, p)));
-      ke[p] = exp_of(kexp[tiles[p]]);
-      ve[p] = exp_of(vexp[tiles[p]]);
+    for (int n = 0; n < 2; ++n) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        tiles[p] = tile_of(entry_at(row_of(k0 + n * kKeys, p)));
+        ke[p] = exp_of(kexp[tiles[p]]);
+        ve[p] = exp_of(vexp[tiles[p]]);
+      }
+      fetch(k0 + n * kKeys);
+      if (n == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) stage(0, i);
+      }
     }
-    fetch(k0);
 #pragma unroll
-    for (int p = 0; p < NP; ++p) tiles[p] = tile_of(entry_at(row_of(k0 + kKeys, p)));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) stage(0, i);
+    for (int p = 0; p < NP; ++p) tiles[p] = tile_of(entry_at(row_of(k0 + 2 * kKeys, p)));
     __syncthreads();
     for (int base = k0;;) {
       step(std::integral_constant<int, 0>{}, base);

@@ -29,6 +29,7 @@ a paged 8-bit cache (q, k, v [1, heads, tokens, 128], the streams' new tokens pa
 """
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -510,14 +511,21 @@ def fva_attn_fp8v(q, k, v8, vexp, tiling: Tiling, mask, counts=None, kv_idx=None
 _DTYPES = {torch.bfloat16: FVA_BF16, torch.float16: FVA_FP16, torch.float32: FVA_FP32}
 
 
-def _same_device(x, *others):
-    """The calls below run on the current device: tensors of another one are refused."""
+def _same_device(x, *others) -> int:
+    """The calls below run on the current device: tensors of another one are refused. Returns the device."""
     dev = x.get_device()
     if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError("tensors must be on the current device")
     for t in others:
         if t is not None and t.get_device() != dev:
             raise ValueError("tensors must be on one device")
+    return dev
+
+
+def _stream_on(dev: int, stream):
+    """_stream_ptr for a device that is known to be the current one."""
+    raw = None if stream is not None else getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return _stream_ptr(stream) if raw is None else raw(dev)
 
 
 def _int32(t, what, *shape):
@@ -545,7 +553,12 @@ def _empty(make, stream):
 
 
 def _like(x, stream):
-    return _empty(lambda: torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device), stream)
+    """A new tensor with x's strides (empty_like keeps those of dense tensors)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _like(x, None)
+    y = torch.empty_like(x)
+    return y if y.stride() == x.stride() else torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
 
 
 def _matches(out, x):
@@ -563,7 +576,7 @@ def fva_rope(q, k, hw, dims, *, ids=None, origin=(0, 0, 0), theta: float = 10000
     """
     if q.dtype not in _DTYPES or (k is not None and k.dtype != q.dtype):
         raise ValueError("q and k must share one of bf16, fp16 and fp32")
-    _same_device(q, k, ids)
+    dev = _same_device(q, k, ids)
     if out is None:
         q_out, k_out = _like(q, stream), None if k is None else _like(k, stream)
     else:
@@ -585,7 +598,7 @@ def fva_rope(q, k, hw, dims, *, ids=None, origin=(0, 0, 0), theta: float = 10000
     st = lib.fva_rope(
         q.data_ptr(), q_out.data_ptr(), ctypes.byref(qd), _ptr(k), _ptr(k_out),
         None if kd is None else ctypes.byref(kd), _DTYPES[q.dtype], ctypes.byref(params), _ptr(ids), ids_stride,
-        _stream_ptr(stream),
+        _stream_on(dev, stream),
     )
     _check(st, "fva_rope")
     return q_out if k is None else (q_out, k_out)
@@ -597,7 +610,7 @@ def fva_cache_plan(held, fresh, state, ring, block_table, page: int, tokens: int
     held, fresh: int32 [streams]; state: int32 [3]; ring: int32 [ring size]; block_table: int32 [streams, width];
     tokens: rows of the slots and ids. Returns (kv_len, q_start, slots, ids, state).
     """
-    _same_device(held, fresh, state, ring, block_table)
+    dev = _same_device(held, fresh, state, ring, block_table)
     n, tokens = held.numel(), int(tokens)
     _int32(held, "held", n)
     _int32(fresh, "fresh", n)
@@ -619,7 +632,7 @@ def fva_cache_plan(held, fresh, state, ring, block_table, page: int, tokens: int
     st = lib.fva_cache_plan(
         held.data_ptr(), fresh.data_ptr(), n, page, state.data_ptr(), ring.data_ptr(), ring.numel(),
         block_table.data_ptr(), width, tokens, kv_len.data_ptr(), q_start.data_ptr(), slots.data_ptr(), ids.data_ptr(),
-        state_out.data_ptr(), _stream_ptr(stream),
+        state_out.data_ptr(), _stream_on(dev, stream),
     )
     _check(st, "fva_cache_plan")
     return kv_len, q_start, slots, ids, state_out
@@ -647,13 +660,13 @@ def fva_cache_store(k, v, slots, k8, v8, k_exp, v_exp, *, stream=None):
         raise ValueError("k and v must be bf16")
     if k.shape != v.shape or k.stride() != v.stride():
         raise ValueError("k and v must share shape and strides")
-    _same_device(k, v, slots, k8, v8, k_exp, v_exp)
+    dev = _same_device(k, v, slots, k8, v8, k_exp, v_exp)
     desc = _rows_of(k)
     if slots.dtype is not torch.int32 or slots.numel() != desc.batch * desc.tokens or not slots.is_contiguous():
         raise ValueError("slots must be a contiguous int32 tensor with one entry per (batch, token)")
     cache = _cache_of(k8, v8, k_exp, v_exp)
     st = lib.fva_cache_store(k.data_ptr(), v.data_ptr(), ctypes.byref(desc), slots.data_ptr(), ctypes.byref(cache),
-                             _stream_ptr(stream))
+                             _stream_on(dev, stream))
     _check(st, "fva_cache_store")
 
 
@@ -667,6 +680,15 @@ def fva_attn_cache_workspace_size(desc: _Desc, cache: _Cache, table_width: int, 
     return n.value
 
 
+@functools.lru_cache(maxsize=4096)
+def _attn_cache_bytes(heads, tokens, kv_heads, page, width, streams, max_q) -> int:
+    """The workspace query by the sizes that it depends on (the call itself checks everything else)."""
+    one = 16  # any aligned address: the query looks at sizes alone
+    return fva_attn_cache_workspace_size(
+        _Desc(1, heads, tokens, 128, 0, tokens * 128, 128), _Cache(1, kv_heads, page, 128, one, one, one, one), width,
+        streams, max_q)
+
+
 def fva_attn_cache(q, k8, v8, k_exp, v_exp, block_table, kv_len, q_start, max_q: int, *, frame: int = 0,
                    window: int = 0, scale: float = 0.0, out=None, workspace=None, stream=None):
     """Attention of the streams' newest tokens over their cached ones (see include/fva.h). Returns O.
@@ -676,7 +698,7 @@ def fva_attn_cache(q, k8, v8, k_exp, v_exp, block_table, kv_len, q_start, max_q:
     """
     if q.dtype != torch.bfloat16:
         raise ValueError("q must be bf16")
-    _same_device(q, k8, v8, k_exp, v_exp, block_table, kv_len, q_start, out, workspace)
+    dev = _same_device(q, k8, v8, k_exp, v_exp, block_table, kv_len, q_start, out, workspace)
     desc = _rows_of(q)
     cache = _cache_of(k8, v8, k_exp, v_exp)
     n = kv_len.numel()
@@ -688,12 +710,12 @@ def fva_attn_cache(q, k8, v8, k_exp, v_exp, block_table, kv_len, q_start, max_q:
         out = _like(q, stream)
     else:
         _matches(out, q)
-    nbytes = fva_attn_cache_workspace_size(desc, cache, width, n, max_q)
+    nbytes = _attn_cache_bytes(desc.heads, desc.tokens, cache.heads, cache.page, width, n, max_q)
     ws = _empty(lambda: _workspace(nbytes, q.device, workspace), stream) if nbytes else None
     st = lib.fva_attn_cache(
         q.data_ptr(), ctypes.byref(desc), ctypes.byref(cache), block_table.data_ptr(), width, kv_len.data_ptr(),
         q_start.data_ptr(), n, max_q, frame, window, scale, out.data_ptr(), _ptr(ws),
-        0 if ws is None else ws.numel() * ws.element_size(), _stream_ptr(stream),
+        0 if ws is None else ws.numel() * ws.element_size(), _stream_on(dev, stream),
     )
     _check(st, "fva_attn_cache")
     return out

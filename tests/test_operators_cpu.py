@@ -115,7 +115,7 @@ def test_attn_refusals():
         (INV, dict(window=-1)), (INV, dict(scale=float("nan"))), (INV, dict(scale=float("inf"))),
         (SHAPE, dict(d=desc(B=2))), (SHAPE, dict(d=desc(H=3))), (SHAPE, dict(d=desc(sn=0))), (SHAPE, dict(width=0)),
         (SHAPE, dict(streams=-1)), (UNS, dict(d=desc(D=64))), (UNS, dict(width=1 << 24)),
-        (WS, dict(ws=None)), (WS, dict(nbytes=100)), (WS, dict(ws=A + 128)),
+        (WS, dict(width=100, ws=None)), (WS, dict(width=100, nbytes=100)), (WS, dict(width=100, ws=A + 128)),
     ]:
         assert attn(**kw) == want, kw
     assert attn(q=None, o=None, d=desc(N=0)) == fva.FVA_OK

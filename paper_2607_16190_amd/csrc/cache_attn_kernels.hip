@@ -37,6 +37,8 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kRows = 16;        // query rows of a small tile: one MFMA column each
 constexpr int kBigRows = 128;    // query rows of a large tile: 32 for each wave
@@ -45,7 +47,6 @@ constexpr int kWaves = 4;        // waves of a workgroup, each on every fourth 6
 constexpr int kCacheSlots = 2048; // workgroups to split for, small tiles
 constexpr int kBigSlots = 512;    // large tiles: two a CU, as many as are resident
 constexpr int kXcds = 8;
-constexpr int kFewKeys = 2048;    // streams up to which a small tile's keys stay in one workgroup
 constexpr int kMinChunk = kWaves * kKeys;  // a shorter chunk leaves waves without keys
 
 // One stream's share of the work: its rows, keys and tiles.
@@ -247,6 +248,12 @@ __device__ __forceinline__ float sum4(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+template <bool STREAM, typename V>
+__device__ __forceinline__ V load(const uint8_t* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  return *reinterpret_cast<const V*>(p);
+}
+
 // One tile of query rows against one chunk of its keys.
 //
 // Operand layouts (16x16x32 products; lane = 16 g + l). S^T = K Q^T: lane (g, l) holds key
@@ -257,7 +264,7 @@ __device__ __forceinline__ float sum4(float v) {
 // of each of the eight rows; a byte permute of two rows' words puts two keys of one
 // channel side by side, as the conversion takes them. Tile m of O^T holds channel 8 l + m,
 // so a lane ends with eight consecutive channels of a query row per accumulator index.
-template <int WAVES>
+template <int WAVES, bool STREAM>
 __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnArgs P) {
   __shared__ __align__(16) float ot[WAVES][kRows][kHeadDim + 4];
   __shared__ float ms[WAVES][kRows], ls[WAVES][kRows];
@@ -306,8 +313,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
   for (int base = k0 + wave * kKeys; base < k1; base += WAVES * kKeys) {
     // Keys outside [lo, k1) repeat the nearest one inside: their pages may be no
     // longer the stream's, and their codes anything.
-    uint4 kraw[4][2];
-    uint2 vraw[4][4];
+    u32x4 kraw[4][2];
+    u32x2 vraw[4][4];
     float ke[4], ve[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -319,12 +326,12 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
       const uint8_t* kp = P.k8 + at * P.page * kHeadDim;
       const uint8_t* vp = P.v8 + at * P.page * kHeadDim;
       const int kr = min(max(base + 16 * t + l, it.lo), k1 - 1) & (P.page - 1);
-      kraw[t][0] = *reinterpret_cast<const uint4*>(kp + kr * kHeadDim + 16 * g);
-      kraw[t][1] = *reinterpret_cast<const uint4*>(kp + kr * kHeadDim + 64 + 16 * g);
+      kraw[t][0] = load<STREAM, u32x4>(kp + kr * kHeadDim + 16 * g);
+      kraw[t][1] = load<STREAM, u32x4>(kp + kr * kHeadDim + 64 + 16 * g);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int vr = min(max(base + 16 * t + 4 * g + r, it.lo), k1 - 1) & (P.page - 1);
-        vraw[t][r] = *reinterpret_cast<const uint2*>(vp + vr * kHeadDim + 8 * l);
+        vraw[t][r] = load<STREAM, u32x2>(vp + vr * kHeadDim + 8 * l);
       }
     }
     f32x4 s[4];
@@ -383,7 +390,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
         uint32_t lo2[4], hi2[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint2 ra = vraw[2 * b + (j >> 1)][2 * (j & 1)], rb = vraw[2 * b + (j >> 1)][2 * (j & 1) + 1];
+          const u32x2 ra = vraw[2 * b + (j >> 1)][2 * (j & 1)], rb = vraw[2 * b + (j >> 1)][2 * (j & 1) + 1];
           const uint32_t a = w ? ra.y : ra.x, c = w ? rb.y : rb.x;
           lo2[j] = __builtin_amdgcn_perm(c, a, 0x05010400u);
           hi2[j] = __builtin_amdgcn_perm(c, a, 0x07030602u);
@@ -415,35 +422,36 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
     ls[wave][l] = lsum;
   }
   __syncthreads();
-  // Thread: row threadIdx / 16, channels 8 (threadIdx % 16) .. + 7.
-  if (threadIdx.x >= 16 * kRows) return;
-  const int orow = threadIdx.x >> 4, oc = 8 * (threadIdx.x & 15);
-  const int out_row = tile * kRows + orow;
-  if (out_row >= st.q_len * P.group) return;
-  float m = ms[0][orow];
+  // Eight channels of a row per thread and turn.
+  for (int piece = threadIdx.x; piece < 16 * kRows; piece += WAVES * kWave) {
+    const int orow = piece >> 4, oc = 8 * (piece & 15);
+    const int out_row = tile * kRows + orow;
+    if (out_row >= st.q_len * P.group) break;
+    float m = ms[0][orow];
 #pragma unroll
-  for (int w = 1; w < WAVES; ++w) m = fmaxf(m, ms[w][orow]);
-  float sum = 0.f;
-  f32x8 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, ms[w][orow]);
+    float sum = 0.f;
+    f32x8 acc = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    const float f = __builtin_amdgcn_exp2f(ms[w][orow] - m);
-    sum += f * ls[w][orow];
+    for (int w = 0; w < WAVES; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ms[w][orow] - m);
+      sum += f * ls[w][orow];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] += f * ot[w][orow][oc + e];
-  }
-  if (n_chunks == 1) {
-    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
-    const int ot_tok = out_row / P.group;
-    const int oh = kh * P.group + out_row - ot_tok * P.group;
-    uint16_t* dst = static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + ot_tok) * P.stride_n + (int64_t)oh * P.stride_h + oc;
-    *reinterpret_cast<bf16x8*>(dst) = __builtin_convertvector(acc * inv, bf16x8);
-  } else {
-    float* part = P.partial + ((int64_t)item * P.kv_heads + kh) * (kRows * (kHeadDim + 2));
-    *reinterpret_cast<f32x8*>(part + orow * kHeadDim + oc) = acc;
-    if (oc == 0) {
-      part[kRows * kHeadDim + orow] = m;
-      part[kRows * kHeadDim + kRows + orow] = sum;
+      for (int e = 0; e < 8; ++e) acc[e] += f * ot[w][orow][oc + e];
+    }
+    if (n_chunks == 1) {
+      const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+      const int out_tok = out_row / P.group;
+      const int oh = kh * P.group + out_row - out_tok * P.group;
+      uint16_t* dst = static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + out_tok) * P.stride_n + (int64_t)oh * P.stride_h + oc;
+      *reinterpret_cast<bf16x8*>(dst) = __builtin_convertvector(acc * inv, bf16x8);
+    } else {
+      float* part = P.partial + ((int64_t)item * P.kv_heads + kh) * (kRows * (kHeadDim + 2));
+      *reinterpret_cast<f32x8*>(part + orow * kHeadDim + oc) = acc;
+      if (oc == 0) {
+        part[kRows * kHeadDim + orow] = m;
+        part[kRows * kHeadDim + kRows + orow] = sum;
+      }
     }
   }
 }
@@ -973,6 +981,9 @@ struct Sizes {
   int rows, slots;
   int64_t tiles, items;
 };
+// Streams of few keys stay in one workgroup a tile: up to four turns of eight waves.
+bool few_keys(int64_t most_keys) { return most_keys <= 2048; }
+
 Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
   const int group = heads / kv_heads;
   Sizes r;
@@ -984,8 +995,8 @@ Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int max_q, int6
   const int round = std::max(1, (r.big ? kBigSlots : kCacheSlots) / kv_heads);
   const int64_t full = ((int64_t)tokens * group + r.rows - 1) / r.rows;  // tiles if the rows fill them
   // From two rounds of tiles on their own, chunks no longer pay for the merge.
-  // Nor do they where eight waves go through the keys in four turns of 64 or fewer.
-  const bool few = most_keys <= (r.big ? kMinChunk : kFewKeys);
+  // Nor do they where keys are few.
+  const bool few = r.big ? most_keys <= kMinChunk : few_keys(most_keys);
   r.slots = few || full >= 2 * (int64_t)round ? 0 : (full > round ? 2 : 1) * round;
   // The sum of chunks_of(mean) is at most slots + tiles, and chunks_of(span) at most twice
   // that, equal where the mean is the span (always for small tiles).
@@ -1005,26 +1016,44 @@ size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int strea
   return z.slots ? (size_t)z.items * kv_heads * z.rows * (kHeadDim + 2) * sizeof(float) : 0;
 }
 
+namespace {
+template <int WAVES, bool STREAM>
+void launch_small(const CacheAttnArgs& a) {
+  cache_attn_kernel<WAVES, STREAM><<<(unsigned)a.items, WAVES * kWave, 0, a.stream>>>(a);
+}
+}  // namespace
+
 hipError_t launch_cache_attn(CacheAttnArgs a) {
   (void)hipGetLastError();
   if (a.tokens == 0 || a.heads == 0 || a.streams == 0) return hipSuccess;
   a.group = a.heads / a.kv_heads;
-  const Sizes z = sizes_of(a.tokens, a.heads, a.kv_heads, a.streams, a.max_q, (int64_t)a.width * a.page);
+  const int64_t most_keys = (int64_t)a.width * a.page;
+  const Sizes z = sizes_of(a.tokens, a.heads, a.kv_heads, a.streams, a.max_q, most_keys);
   a.rows = z.rows;
   a.row_shift = z.big ? 7 : 4;
   a.ramp = z.big && a.frame;
   a.slots = z.slots;
   a.inv_slots = z.slots ? 1.0 / z.slots : 0.0;
   a.items = z.items * a.kv_heads;
+  // Small tiles of few keys: as many waves a tile as the chip has room for (twelve a CU) when
+  // all tiles run at once. Of many keys: four, and the codes, which no other workgroup of
+  // the call reads, past the caches (64 ragged streams of up to 16000 keys, 8 heads: 165 ->
+  // 154 us; 111,600 keys of 40 heads: 207 -> 190, 6.0 TB/s).
   const unsigned grid = (unsigned)((a.items + kXcds - 1) / kXcds * kXcds);
   if (z.big && a.page >= kKeys)
     cache_attn_big_kernel<true><<<grid, kWaves * kWave, 0, a.stream>>>(a);
   else if (z.big)
     cache_attn_big_kernel<false><<<grid, kWaves * kWave, 0, a.stream>>>(a);
-  else if (!z.slots)
-    cache_attn_kernel<2 * kWaves><<<(unsigned)a.items, 2 * kWaves * kWave, 0, a.stream>>>(a);
+  else if (few_keys(most_keys) && a.items <= 384)
+    launch_small<8, false>(a);
+  else if (few_keys(most_keys) && a.items > 1536)
+    launch_small<1, false>(a);
+  else if (few_keys(most_keys) && a.items > 768)
+    launch_small<2, false>(a);
+  else if (few_keys(most_keys))
+    launch_small<4, false>(a);
   else
-    cache_attn_kernel<kWaves><<<(unsigned)a.items, kWaves * kWave, 0, a.stream>>>(a);
+    launch_small<4, true>(a);
   if (z.slots) cache_combine_kernel<<<(unsigned)(z.tiles * a.kv_heads * (z.rows / 16)), 256, 0, a.stream>>>(a);
   return hipGetLastError();
 }

@@ -47,6 +47,7 @@ constexpr int kWaves = 4;        // waves of a workgroup, each on every fourth 6
 constexpr int kCacheSlots = 2048; // workgroups to split for, small tiles
 constexpr int kBigSlots = 512;    // large tiles: two a CU, as many as are resident
 constexpr int kXcds = 8;
+constexpr int kMostChunks = 128;  // of a tile
 constexpr int kMinChunk = kWaves * kKeys;  // a shorter chunk leaves waves without keys
 
 // One stream's share of the work: its rows, keys and tiles.
@@ -79,7 +80,11 @@ struct Span {
   int begin, lo, end;
 };
 
-__device__ __forceinline__ int chunks_of(int span, int chunk) { return max(1, (span + chunk - 1) / chunk); }
+// Chunks that `span` keys are cut into, at least one and at most kMostChunks (their merge
+// takes a turn of its own for every few).
+__device__ __forceinline__ int chunks_of(int span, int chunk) {
+  return min(max(1, (span + chunk - 1) / chunk), kMostChunks);
+}
 
 // What a wave knows of the whole call: the streams over its lanes, the first 64 of them
 // in registers (the others are looked at again).
@@ -870,12 +875,12 @@ __device__ __forceinline__ float wave_reduce(float v, Op op) {
   return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// ROWS rows of a tile from row r on: the partial results of its chunks in chunk order. Lane
-// c has the reference and sum of chunk c (64 chunks at a time), then the chunks' rows are
-// loaded DEPTH chunks at a time for all ROWS rows, all loads independent; lane i has
-// channels 2 i and 2 i + 1. out(row, value) is called for every row.
+// ROWS rows of a tile from row r on: the partial results of its chunks [c_begin, c_end), in
+// chunk order. Lane c has the reference and sum of chunk c (64 chunks at a time), then the
+// chunks' rows are loaded DEPTH chunks at a time for all ROWS rows, all loads independent;
+// lane i has channels 2 i and 2 i + 1. out(i, reference, sum, value) is called for every row.
 template <int ROWS, int DEPTH, typename F>
-__device__ __forceinline__ void merge_rows(const float* base, int64_t step, int tile_rows, int n_chunks, int r, int lane, F&& out) {
+__device__ __forceinline__ void merge_rows(const float* base, int64_t step, int tile_rows, int c_begin, int c_end, int r, int lane, F&& out) {
   float m[ROWS], sum[ROWS];
   float2 acc[ROWS];
 #pragma unroll
@@ -884,8 +889,8 @@ __device__ __forceinline__ void merge_rows(const float* base, int64_t step, int 
     sum[i] = 0.f;
     acc[i] = make_float2(0.f, 0.f);
   }
-  for (int c0 = 0; c0 < n_chunks; c0 += kWave) {
-    const int n = min(n_chunks - c0, kWave);
+  for (int c0 = c_begin; c0 < c_end; c0 += kWave) {
+    const int n = min(c_end - c0, kWave);
     const float* at = base + (int64_t)(c0 + min(lane, n - 1)) * step + tile_rows * kHeadDim + r;
     float w[ROWS], pl[ROWS];
 #pragma unroll
@@ -926,15 +931,15 @@ __device__ __forceinline__ void merge_rows(const float* base, int64_t step, int 
     }
   }
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    const float inv = sum[i] > 0.f ? 1.0f / sum[i] : 0.f;
-    out(r + i, make_float2(acc[i].x * inv, acc[i].y * inv));
-  }
+  for (int i = 0; i < ROWS; ++i) out(i, m[i], sum[i], acc[i]);
 }
 
-// 16 rows of a tile per workgroup, four per wave at once; a wave with one row (single
-// tokens: many chunks) takes more of its chunks at once.
+// 16 rows of a tile per workgroup, four per wave at once. Where there are few rows and many
+// chunks (single tokens), the waves share the chunks instead and meet in LDS: 71,900 keys
+// of one K/V head, four query heads: 66 us with each wave on rows of its own, 29 so.
 __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
+  __shared__ float2 acc_s[4][4][kWave];
+  __shared__ float m_s[4][4], sum_s[4][4];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int parts = P.rows / 16;
@@ -956,22 +961,51 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   const float* base = P.partial + first * size;
   const int64_t step = P.kv_heads * size;
   const int rows = st.q_len * P.group;
-  auto out = [&](int r, float2 o) {
+  auto put = [&](int r, float sum, float2 o) {
     const int row = tile * P.rows + r;
     if (row >= rows) return;
+    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
     const int tok = row / P.group;
     const int qh = kh * P.group + row - tok * P.group;
     bf16x2 v;
-    v[0] = (__bf16)o.x;
-    v[1] = (__bf16)o.y;
+    v[0] = (__bf16)(o.x * inv);
+    v[1] = (__bf16)(o.y * inv);
     *reinterpret_cast<bf16x2*>(static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + tok) * P.stride_n + (int64_t)qh * P.stride_h + 2 * lane) = v;
   };
-  const int r = 16 * part + 4 * wave;
-  const int left = rows - (tile * P.rows + r);
-  if (left > 1)
-    merge_rows<4, 4>(base, step, P.rows, n_chunks, r, lane, out);
-  else if (left == 1)
-    merge_rows<1, 16>(base, step, P.rows, n_chunks, r, lane, out);
+  const int r0 = 16 * part;
+  const int left = rows - (tile * P.rows + r0);  // real rows from the part's first on
+  if (left > 8 || n_chunks <= 8) {
+    const int r = r0 + 4 * wave;
+    if (left > 4 * wave)
+      merge_rows<4, 4>(base, step, P.rows, 0, n_chunks, r, lane, [&](int i, float, float sum, float2 o) { put(r + i, sum, o); });
+    return;
+  }
+  const int share = (n_chunks + 3) / 4;
+  for (int g0 = 0; g0 < left; g0 += 4) {
+    merge_rows<4, 4>(base, step, P.rows, min(wave * share, n_chunks), min((wave + 1) * share, n_chunks), r0 + g0, lane,
+                     [&](int i, float m, float sum, float2 o) {
+                       acc_s[wave][i][lane] = o;
+                       if (lane == 0) {
+                         m_s[wave][i] = m;
+                         sum_s[wave][i] = sum;
+                       }
+                     });
+    __syncthreads();
+    float m = m_s[0][wave];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) m = fmaxf(m, m_s[w][wave]);
+    float sum = 0.f;
+    float2 o = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = __builtin_amdgcn_exp2f(m_s[w][wave] - m);
+      sum = fmaf(f, sum_s[w][wave], sum);
+      o.x = fmaf(f, acc_s[w][wave][lane].x, o.x);
+      o.y = fmaf(f, acc_s[w][wave][lane].y, o.y);
+    }
+    put(r0 + g0 + wave, sum, o);
+    __syncthreads();
+  }
 }
 
 // Which kernel, the workgroups per K/V head to split for (0: the tiles alone fill the
@@ -980,11 +1014,13 @@ struct Sizes {
   bool big;
   int rows, slots;
   int64_t tiles, items;
+  int64_t keys;  // that any tile sees, at most
 };
 // Streams of few keys stay in one workgroup a tile: up to four turns of eight waves.
 bool few_keys(int64_t most_keys) { return most_keys <= 2048; }
 
-Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
+// window, frame: 0 where they are not known.
+Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys, int window, int frame) {
   const int group = heads / kv_heads;
   Sizes r;
   // One small tile per stream reads the keys once, straight into registers. More rows than
@@ -996,7 +1032,10 @@ Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int max_q, int6
   const int64_t full = ((int64_t)tokens * group + r.rows - 1) / r.rows;  // tiles if the rows fill them
   // From two rounds of tiles on their own, chunks no longer pay for the merge.
   // Nor do they where keys are few.
-  const bool few = r.big ? most_keys <= kMinChunk : few_keys(most_keys);
+  if (window) most_keys = std::min(most_keys, (int64_t)window + 2 * (int64_t)frame + r.rows + kKeys);  // as in stream_of
+  r.keys = most_keys;
+  // (large tiles: ten steps are over before a second launch would merge anything)
+  const bool few = r.big ? most_keys <= 10 * kKeys : few_keys(most_keys);
   r.slots = few || full >= 2 * (int64_t)round ? 0 : (full > round ? 2 : 1) * round;
   // The sum of chunks_of(mean) is at most slots + tiles, and chunks_of(span) at most twice
   // that, equal where the mean is the span (always for small tiles).
@@ -1007,12 +1046,12 @@ Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int max_q, int6
 }  // namespace
 
 int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
-  const Sizes z = sizes_of(tokens, heads, kv_heads, streams, max_q, most_keys);
+  const Sizes z = sizes_of(tokens, heads, kv_heads, streams, max_q, most_keys, 0, 0);
   return std::max(z.items, z.tiles * (z.rows / 16)) * kv_heads + kXcds;
 }
 
 size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
-  const Sizes z = sizes_of(tokens, heads, kv_heads, streams, max_q, most_keys);
+  const Sizes z = sizes_of(tokens, heads, kv_heads, streams, max_q, most_keys, 0, 0);
   return z.slots ? (size_t)z.items * kv_heads * z.rows * (kHeadDim + 2) * sizeof(float) : 0;
 }
 
@@ -1027,8 +1066,7 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
   (void)hipGetLastError();
   if (a.tokens == 0 || a.heads == 0 || a.streams == 0) return hipSuccess;
   a.group = a.heads / a.kv_heads;
-  const int64_t most_keys = (int64_t)a.width * a.page;
-  const Sizes z = sizes_of(a.tokens, a.heads, a.kv_heads, a.streams, a.max_q, most_keys);
+  const Sizes z = sizes_of(a.tokens, a.heads, a.kv_heads, a.streams, a.max_q, (int64_t)a.width * a.page, a.window, a.frame);
   a.rows = z.rows;
   a.row_shift = z.big ? 7 : 4;
   a.ramp = z.big && a.frame;
@@ -1044,13 +1082,13 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
     cache_attn_big_kernel<true><<<grid, kWaves * kWave, 0, a.stream>>>(a);
   else if (z.big)
     cache_attn_big_kernel<false><<<grid, kWaves * kWave, 0, a.stream>>>(a);
-  else if (few_keys(most_keys) && a.items <= 384)
+  else if (few_keys(z.keys) && a.items <= 384)
     launch_small<8, false>(a);
-  else if (few_keys(most_keys) && a.items > 1536)
+  else if (few_keys(z.keys) && a.items > 1536)
     launch_small<1, false>(a);
-  else if (few_keys(most_keys) && a.items > 768)
+  else if (few_keys(z.keys) && a.items > 768)
     launch_small<2, false>(a);
-  else if (few_keys(most_keys))
+  else if (few_keys(z.keys))
     launch_small<4, false>(a);
   else
     launch_small<4, true>(a);

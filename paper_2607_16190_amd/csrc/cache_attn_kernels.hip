@@ -50,6 +50,11 @@ constexpr int kXcds = 8;
 constexpr int kMostChunks = 128;  // of a tile
 constexpr int kMinChunk = kWaves * kKeys;  // a shorter chunk leaves waves without keys
 
+typedef __attribute__((address_space(4))) const int32_t const_i32;
+
+// n / d for 0 <= n < 2^31 without a division (Divisor).
+__device__ __forceinline__ int divide(int n, const Divisor& d) { return (int)(((uint64_t)(uint32_t)n * d.mul) >> d.shift); }
+
 // One stream's share of the work: its rows, keys and tiles.
 struct Stream {
   int q0, q_len;  // first token row, tokens
@@ -57,6 +62,7 @@ struct Stream {
   int tiles;
   int span;       // keys that any of its tiles sees, at most
   int mean;       // about how many they see in the middle, at least span / 2
+  int chunks;     // that a tile's keys are cut into, at most (set by work_of)
 };
 
 __device__ __forceinline__ Stream stream_of(const CacheAttnArgs& P, int s) {
@@ -65,12 +71,11 @@ __device__ __forceinline__ Stream stream_of(const CacheAttnArgs& P, int s) {
   // tensors whatever they hold.
   r.q0 = min(max(P.q_start[s], 0), P.tokens);
   r.q_len = min(max(P.q_start[s + 1], r.q0), P.tokens) - r.q0;
-  r.kv_len = (int)min((int64_t)max(P.kv_len[s], 0), (int64_t)P.width * P.page);
-  r.tiles = (int)((((int64_t)r.q_len * P.group) + P.rows - 1) >> P.row_shift);
-  int64_t span = r.kv_len;
-  if (P.window) span = min(span, (int64_t)P.window + 2 * (int64_t)P.frame + P.rows + kKeys);
-  r.span = (int)span;
-  r.mean = P.ramp ? (int)min(span, max((int64_t)r.kv_len - (r.q_len >> 1), (int64_t)((r.kv_len + 1) >> 1))) : r.span;
+  r.kv_len = min(max(P.kv_len[s], 0), P.width << P.page_shift);
+  r.tiles = (int)(((uint32_t)(r.q_len * P.group) + (uint32_t)P.rows - 1) >> P.row_shift);
+  r.span = min(r.kv_len, P.most_keys);
+  r.mean = P.ramp ? min(r.span, max(r.kv_len - (r.q_len >> 1), (r.kv_len + 1) >> 1)) : r.span;
+  r.chunks = 1;
   return r;
 }
 
@@ -83,94 +88,103 @@ struct Span {
 // Chunks that `span` keys are cut into, at least one and at most kMostChunks (their merge
 // takes a turn of its own for every few).
 __device__ __forceinline__ int chunks_of(int span, int chunk) {
-  return min(max(1, (span + chunk - 1) / chunk), kMostChunks);
+  return (int)min(max(1u, ((uint32_t)span + (uint32_t)chunk - 1u) / (uint32_t)chunk), (uint32_t)kMostChunks);
 }
 
 // What a wave knows of the whole call: the streams over its lanes, the first 64 of them
 // in registers (the others are looked at again).
 struct Work {
   Stream mine;
-  int chunk;  // keys of a chunk, at most
+  int chunk;     // keys of a chunk, at most
+  int upto;      // items of the first 64 streams up to and with the lane's
+  int items;     // of all, per K/V head
 };
 
-template <typename F>
-__device__ __forceinline__ void each_stream(const CacheAttnArgs& P, const Stream& mine, int lane, F&& f) {
-  f(mine);
-  for (int s = lane + kWave; s < P.streams; s += kWave) f(stream_of(P, s));
+__device__ __forceinline__ Stream none() { return Stream{0, 0, 0, 0, 0, 0, 1}; }
+
+__device__ __forceinline__ Stream stream_in(const CacheAttnArgs& P, int s, int chunk) {
+  if (s >= P.streams) return none();
+  Stream r = stream_of(P, s);
+  if (P.slots) r.chunks = chunks_of(r.span, chunk);
+  return r;
 }
 
 // Longest chunk: the tiles' keys over the P.slots workgroups there are to fill. Large tiles
 // run in rounds of as many workgroups as are resident, so theirs grows until the chunks fit
 // the rounds (a few left over would take a round of their own). A stream's keys are then
-// cut into equal chunks of at most that (chunk_of).
+// cut into equal chunks of at most that (chunk_keys). Every sum is of integers: each wave of
+// both kernels comes to the same numbers.
 __device__ __forceinline__ Work work_of(const CacheAttnArgs& P, int lane) {
   constexpr int kNever = INT32_MAX / 2;
   Work w;
-  w.mine = Stream{0, 0, 0, 0, 0, 0};
-  if (lane < P.streams) w.mine = stream_of(P, lane);
+  w.mine = lane < P.streams ? stream_of(P, lane) : none();
   w.chunk = kNever;
-  if (P.slots > 0) {
-    uint64_t total = 0;
-    each_stream(P, w.mine, lane, [&](const Stream& r) { total += (uint64_t)r.tiles * (uint64_t)r.mean; });
+  if (P.slots) {
+    uint64_t total = (uint64_t)w.mine.tiles * (uint64_t)w.mine.mean;
+    for (int s = lane + kWave; s < P.streams; s += kWave) {
+      const Stream r = stream_of(P, s);
+      total += (uint64_t)r.tiles * (uint64_t)r.mean;
+    }
     total = wave_sum_u64(total);
     const double units = ceil((double)total * P.inv_slots * (1.0 / kKeys));
     if (units < kNever / kKeys / 8) {
       int n = max((int)units, kMinChunk / kKeys);
       for (int tries = 0; P.rows == kBigRows && tries < 10; ++tries) {
-        uint64_t items = 0;
-        each_stream(P, w.mine, lane, [&](const Stream& r) { items += (uint64_t)r.tiles * (uint64_t)chunks_of(r.mean, n * kKeys); });
+        uint64_t items = (uint64_t)w.mine.tiles * (uint64_t)chunks_of(w.mine.mean, n * kKeys);
+        for (int s = lane + kWave; s < P.streams; s += kWave) {
+          const Stream r = stream_of(P, s);
+          items += (uint64_t)r.tiles * (uint64_t)chunks_of(r.mean, n * kKeys);
+        }
         if (wave_sum_u64(items) <= (uint64_t)P.slots) break;
         n += max(n >> 3, 1);
       }
       w.chunk = n * kKeys;
     }
+    w.mine.chunks = chunks_of(w.mine.span, w.chunk);
+  }
+  w.upto = wave_incl_scan_i32(w.mine.tiles * w.mine.chunks, lane);
+  w.items = __builtin_amdgcn_readlane(w.upto, 63);
+  for (int s0 = kWave; s0 < P.streams; s0 += kWave) {
+    const Stream r = stream_in(P, s0 + lane, w.chunk);
+    w.items += __builtin_amdgcn_readlane(wave_incl_scan_i32(r.tiles * r.chunks, lane), 63);
   }
   return w;
 }
 
-// A stream's chunk: as many as w.chunk asks for, of equal length in whole steps of the
-// workgroup's waves (fewer where the steps are long: chunks_of(span, chunk_of) is at most
-// chunks_of(span, w.chunk)).
-__device__ __forceinline__ int chunk_of(const CacheAttnArgs& P, const Stream& r, int chunk) {
-  const int n = chunks_of(r.span, chunk);
-  if (n == 1) return chunk;
-  const int unit = P.rows == kBigRows ? kKeys : kMinChunk;
-  return ((r.span + n - 1) / n + unit - 1) / unit * unit;
+// Keys of a chunk of a stream that is cut into several: equal ones, in whole steps of the
+// workgroup's waves (so a tile may need fewer than st.chunks).
+__device__ __forceinline__ int chunk_keys(const CacheAttnArgs& P, const Stream& st) {
+  const uint32_t unit = P.rows == kBigRows ? kKeys : kMinChunk;  // powers of two
+  const uint32_t even = ((uint32_t)st.span + (uint32_t)st.chunks - 1) / (uint32_t)st.chunks;
+  return (int)((even + unit - 1) & ~(unit - 1));
 }
 
-// All items, per K/V head (starts that are not ascending could ask for more than there is
-// room for).
-__device__ __forceinline__ int items_of(const CacheAttnArgs& P, const Work& w, int lane) {
-  uint64_t n = 0;
-  each_stream(P, w.mine, lane, [&](const Stream& r) { n += (uint64_t)r.tiles * (uint64_t)chunks_of(r.span, w.chunk); });
-  return (int)min(wave_sum_u64(n), (uint64_t)(P.items / P.kv_heads));
+__device__ __forceinline__ Stream lane_stream(const Stream& r, int l) {
+  return Stream{__builtin_amdgcn_readlane(r.q0, l),   __builtin_amdgcn_readlane(r.q_len, l), __builtin_amdgcn_readlane(r.kv_len, l),
+                __builtin_amdgcn_readlane(r.tiles, l), __builtin_amdgcn_readlane(r.span, l),  __builtin_amdgcn_readlane(r.mean, l),
+                __builtin_amdgcn_readlane(r.chunks, l)};
 }
 
-// The stream whose share holds number `at` of the numbers count(stream) of all streams
-// one after the other, -1 for none; `before`: the sum of count before it, `items`: the
-// items before it, `st`: the stream.
-template <typename F>
-__device__ __forceinline__ int find_share(const CacheAttnArgs& P, const Work& w, int lane, int at, F&& count, int& before, int& items, Stream& st) {
-  before = items = 0;
-  Stream r = w.mine;
-  for (int s0 = 0; s0 < P.streams; s0 += kWave) {
-    if (s0) r = s0 + lane < P.streams ? stream_of(P, s0 + lane) : Stream{0, 0, 0, 0, 0, 0};
-    const int c = count(r), n = r.tiles * chunks_of(r.span, w.chunk);
-    const int ci = wave_incl_scan_i32(c, lane), ni = wave_incl_scan_i32(n, lane);
-    const uint64_t past = __ballot(before + ci > at);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      before += __builtin_amdgcn_readlane(ci - c, l);
-      items += __builtin_amdgcn_readlane(ni - n, l);
-      st = Stream{__builtin_amdgcn_readlane(r.q0, l), __builtin_amdgcn_readlane(r.q_len, l),
-                  __builtin_amdgcn_readlane(r.kv_len, l), __builtin_amdgcn_readlane(r.tiles, l),
-                  __builtin_amdgcn_readlane(r.span, l), __builtin_amdgcn_readlane(r.mean, l)};
-      return s0 + l;
-    }
-    before += __builtin_amdgcn_readlane(ci, 63);
-    items += __builtin_amdgcn_readlane(ni, 63);
-  }
-  return -1;
+// Keys [lo, hi) that token i of a stream sees.
+__device__ __forceinline__ void visible(const CacheAttnArgs& P, const Stream& st, int i, int& lo, int& hi) {
+  const int p = st.kv_len - st.q_len + i;
+  int64_t end = st.kv_len;
+  if (P.frame) end = p < 0 ? 0 : ((int64_t)divide(p, P.by_frame) + 1) * P.frame;
+  hi = (int)min(end, (int64_t)st.kv_len);
+  lo = P.window ? (int)max(end - P.window, (int64_t)0) : 0;
+}
+
+__device__ __forceinline__ Span tile_span(const CacheAttnArgs& P, const Stream& st, int tile) {
+  const int row0 = tile << P.row_shift;
+  const int row1 = min(row0 + P.rows, st.q_len * P.group) - 1;
+  int lo, hi, lo1, hi1;
+  visible(P, st, divide(row0, P.by_group), lo, hi);
+  visible(P, st, divide(row1, P.by_group), lo1, hi1);
+  Span r;
+  r.lo = lo;
+  r.begin = lo & ~(kKeys - 1);
+  r.end = hi1 > lo ? hi1 : r.begin;  // no key at all: an empty span
+  return r;
 }
 
 // A work item: a tile's chunk, keys [k0, k1).
@@ -180,47 +194,50 @@ struct Item {
   int tile, n_chunks, k0, k1;
   int lo;      // first key that any row sees
 };
-__device__ __forceinline__ Span tile_span(const CacheAttnArgs& P, const Stream& st, int tile);
 __device__ __forceinline__ Item item_of(const CacheAttnArgs& P, const Work& w, int item, int lane) {
   Item r;
-  int before, items;
-  r.stream = find_share(P, w, lane, item, [&](const Stream& s) { return s.tiles * chunks_of(s.span, w.chunk); }, before, items, r.st);
+  r.stream = -1;
+  int before = 0;  // items of the streams before the one that is found
+  for (int s0 = 0; s0 < P.streams; s0 += kWave) {
+    const Stream mine = s0 ? stream_in(P, s0 + lane, w.chunk) : w.mine;
+    const int upto = s0 ? wave_incl_scan_i32(mine.tiles * mine.chunks, lane) : w.upto;
+    const uint64_t past = __ballot(before + upto > item);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      r.stream = s0 + l;
+      r.st = lane_stream(mine, l);
+      before += __builtin_amdgcn_readlane(upto, l) - r.st.tiles * r.st.chunks;
+      break;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
   if (r.stream < 0) return r;
-  const int keys = chunk_of(P, r.st, w.chunk);
-  const int per_tile = chunks_of(r.st.span, w.chunk);
-  r.tile = (item - items) / per_tile;
-  const int chunk = (item - items) - r.tile * per_tile;
-  const Span span = tile_span(P, r.st, r.tile);
-  r.n_chunks = chunks_of(span.end - span.begin, keys);
-  if (chunk >= r.n_chunks) {  // this tile sees fewer keys than the stream's widest
+  const int at = item - before;
+  int chunk = 0;
+  r.tile = at;
+  if (r.st.chunks > 1) {
+    r.tile = (int)((uint32_t)at / (uint32_t)r.st.chunks);
+    chunk = at - r.tile * r.st.chunks;
+  }
+  if (at < 0 || r.tile >= r.st.tiles) {  // (sums past 32 bits, from starts that are not ascending)
     r.stream = -1;
     return r;
   }
+  const Span span = tile_span(P, r.st, r.tile);
   r.lo = span.lo;
-  r.k0 = (int)min((int64_t)span.begin + (int64_t)chunk * keys, (int64_t)span.end);
-  r.k1 = (int)min((int64_t)r.k0 + keys, (int64_t)span.end);
-  return r;
-}
-
-// Keys [lo, hi) that token i of a stream sees.
-__device__ __forceinline__ void visible(const CacheAttnArgs& P, const Stream& st, int i, int& lo, int& hi) {
-  const int p = st.kv_len - st.q_len + i;
-  int64_t end = st.kv_len;
-  if (P.frame) end = p < 0 ? 0 : ((int64_t)(p / P.frame) + 1) * P.frame;
-  hi = (int)min(end, (int64_t)st.kv_len);
-  lo = P.window ? (int)max(end - P.window, (int64_t)0) : 0;
-}
-
-__device__ __forceinline__ Span tile_span(const CacheAttnArgs& P, const Stream& st, int tile) {
-  const int row0 = tile * P.rows;
-  const int row1 = min(row0 + P.rows, st.q_len * P.group) - 1;
-  int lo, hi, lo1, hi1;
-  visible(P, st, row0 / P.group, lo, hi);
-  visible(P, st, row1 / P.group, lo1, hi1);
-  Span r;
-  r.lo = lo;
-  r.begin = lo & ~(kKeys - 1);
-  r.end = hi1 > lo ? hi1 : r.begin;  // no key at all: an empty span
+  r.k0 = span.begin;
+  r.k1 = span.end;
+  r.n_chunks = 1;
+  if (r.st.chunks > 1) {
+    const int keys = chunk_keys(P, r.st);
+    r.n_chunks = chunks_of(span.end - span.begin, keys);
+    if (chunk >= r.n_chunks) {  // this tile sees fewer keys than the stream's widest
+      r.stream = -1;
+      return r;
+    }
+    r.k0 = (int)min((int64_t)span.begin + (int64_t)chunk * keys, (int64_t)span.end);
+    r.k1 = (int)min((int64_t)r.k0 + keys, (int64_t)span.end);
+  }
   return r;
 }
 
@@ -276,8 +293,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, l = lane & 15;
-  const int kh = blockIdx.x % P.kv_heads;
-  const int item = blockIdx.x / P.kv_heads;
+  const int item = divide(blockIdx.x, P.by_heads);
+  const int kh = (int)blockIdx.x - item * P.kv_heads;
   const Work work = work_of(P, lane);
   const Item it = item_of(P, work, item, lane);
   if (it.stream < 0) return;
@@ -287,7 +304,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
   // This lane's query row.
   const int row = tile * kRows + l;
   const bool real = row < st.q_len * P.group;
-  const int tok = real ? row / P.group : 0;
+  const int tok = real ? divide(row, P.by_group) : 0;
   const int qh = kh * P.group + (real ? row - tok * P.group : 0);
   int lo = 0, hi = 0;
   if (real) visible(P, st, tok, lo, hi);
@@ -446,7 +463,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
     }
     if (n_chunks == 1) {
       const float inv = sum > 0.f ? 1.0f / sum : 0.f;
-      const int out_tok = out_row / P.group;
+      const int out_tok = divide(out_row, P.by_group);
       const int oh = kh * P.group + out_row - out_tok * P.group;
       uint16_t* dst = static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + out_tok) * P.stride_n + (int64_t)oh * P.stride_h + oc;
       *reinterpret_cast<bf16x8*>(dst) = __builtin_convertvector(acc * inv, bf16x8);
@@ -465,7 +482,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) unsigned char lds_u8;
 typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
-typedef __attribute__((address_space(4))) const int32_t const_i32;
 
 template <int B, int E, typename F>
 __device__ __forceinline__ void static_for(F&& f) {
@@ -511,11 +527,11 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   // XCDs in turn): the tiles of a head read its keys out of one L2. Later tiles first: with
   // causal frames they see the most keys.
   const Work work = work_of(P, lane);
-  const int total = items_of(P, work, lane);
+  const int total = (int)min((int64_t)work.items, P.items_per_head);
   const int64_t all = (int64_t)total * P.kv_heads;
   const int64_t run = (all + kXcds - 1) / kXcds;
   const int64_t index = (blockIdx.x % kXcds) * run + blockIdx.x / kXcds;
-  if (blockIdx.x / kXcds >= run || index >= all) return;
+  if (total <= 0 || blockIdx.x / kXcds >= run || index >= all) return;
   const int kh = (int)((uint32_t)index / (uint32_t)total);
   const int item = total - 1 - (int)(index - (int64_t)kh * total);
   const Item it = item_of(P, work, item, lane);
@@ -535,7 +551,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) qf[nt][ks] = bf16x8{};
     if (row < rows) {
-      const int tok = row / P.group;
+      const int tok = divide(row, P.by_group);
       const int qh = kh * P.group + row - tok * P.group;
       visible(P, st, tok, lo[nt], hi[nt]);
       hi[nt] = max(min(hi[nt], k1), lo[nt]);
@@ -842,7 +858,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
     if (row >= rows) continue;
     if (n_chunks == 1) {
       const float inv = lsum[nt][0] > 0.f ? 1.0f / lsum[nt][0] : 0.f;
-      const int tok = row / P.group;
+      const int tok = divide(row, P.by_group);
       const int qh = kh * P.group + row - tok * P.group;
       uint16_t* out = static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + tok) * P.stride_n + (int64_t)qh * P.stride_h + 4 * g;
 #pragma unroll
@@ -942,21 +958,38 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   __shared__ float m_s[4][4], sum_s[4][4];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int parts = P.rows / 16;
-  const int part = blockIdx.x % parts;
-  const int kh = blockIdx.x / parts % P.kv_heads;
-  const int tile_id = blockIdx.x / parts / P.kv_heads;
+  const int part_shift = P.row_shift - 4;
+  const int part = blockIdx.x & ((1 << part_shift) - 1);
+  const int tile_id = divide(blockIdx.x >> part_shift, P.by_heads);
+  const int kh = (int)(blockIdx.x >> part_shift) - tile_id * P.kv_heads;
   const Work work = work_of(P, lane);
-  int before, item0;
+  // the stream that holds tile tile_id, its first tile and its first item
+  int tiles = 0, item0 = 0, stream = -1;
   Stream st;
-  const int stream = find_share(P, work, lane, tile_id, [](const Stream& s) { return s.tiles; }, before, item0, st);
-  if (stream < 0) return;
-  const int tile = tile_id - before;
+  for (int s0 = 0; s0 < P.streams; s0 += kWave) {
+    const Stream mine = s0 ? stream_in(P, s0 + lane, work.chunk) : work.mine;
+    const int upto = s0 ? wave_incl_scan_i32(mine.tiles * mine.chunks, lane) : work.upto;
+    const int tiles_upto = wave_incl_scan_i32(mine.tiles, lane);
+    const uint64_t past = __ballot(tiles + tiles_upto > tile_id);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      stream = s0 + l;
+      st = lane_stream(mine, l);
+      tiles += __builtin_amdgcn_readlane(tiles_upto, l) - st.tiles;
+      item0 += __builtin_amdgcn_readlane(upto, l) - st.tiles * st.chunks;
+      break;
+    }
+    tiles += __builtin_amdgcn_readlane(tiles_upto, 63);
+    item0 += __builtin_amdgcn_readlane(upto, 63);
+  }
+  if (stream < 0 || st.chunks == 1) return;
+  const int tile = tile_id - tiles;
   const Span span = tile_span(P, st, tile);
-  const int n_chunks = chunks_of(span.end - span.begin, chunk_of(P, st, work.chunk));
+  const int n_chunks = chunks_of(span.end - span.begin, chunk_keys(P, st));
   if (n_chunks == 1) return;
-  const int64_t first = (int64_t)(item0 + tile * chunks_of(st.span, work.chunk)) * P.kv_heads + kh;
-  if (first + (int64_t)(n_chunks - 1) * P.kv_heads >= P.items) return;  // starts that are not ascending
+  const int64_t first = ((int64_t)item0 + (int64_t)tile * st.chunks) * P.kv_heads + kh;
+  // (sums past 32 bits, from starts that are not ascending)
+  if (tile < 0 || tile >= st.tiles || item0 < 0 || first + (int64_t)(n_chunks - 1) * P.kv_heads >= P.items) return;
   const int64_t size = P.rows * (kHeadDim + 2);
   const float* base = P.partial + first * size;
   const int64_t step = P.kv_heads * size;
@@ -965,7 +998,7 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
     const int row = tile * P.rows + r;
     if (row >= rows) return;
     const float inv = sum > 0.f ? 1.0f / sum : 0.f;
-    const int tok = row / P.group;
+    const int tok = divide(row, P.by_group);
     const int qh = kh * P.group + row - tok * P.group;
     bf16x2 v;
     v[0] = (__bf16)(o.x * inv);
@@ -1056,6 +1089,15 @@ size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int strea
 }
 
 namespace {
+// n / d = n * mul >> shift for 0 <= n < 2^31: mul = ceil(2^shift / d), shift = 31 + ceil(log2 d)
+// (its error, below n / 2^shift, cannot reach the next multiple of 1 / d).
+Divisor divisor_of(int d) {
+  int up = 0;
+  while (((int64_t)1 << up) < d) ++up;
+  const int shift = 31 + up;
+  return {(uint32_t)((((uint64_t)1 << shift) + (uint32_t)d - 1) / (uint32_t)d), shift};
+}
+
 template <int WAVES, bool STREAM>
 void launch_small(const CacheAttnArgs& a) {
   cache_attn_kernel<WAVES, STREAM><<<(unsigned)a.items, WAVES * kWave, 0, a.stream>>>(a);
@@ -1070,6 +1112,11 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
   a.rows = z.rows;
   a.row_shift = z.big ? 7 : 4;
   a.ramp = z.big && a.frame;
+  a.most_keys = (int)std::min<int64_t>(z.keys, INT32_MAX);
+  a.by_group = divisor_of(a.group);
+  a.by_heads = divisor_of(a.kv_heads);
+  a.by_frame = divisor_of(std::max(a.frame, 1));
+  a.items_per_head = z.items;
   a.slots = z.slots;
   a.inv_slots = z.slots ? 1.0 / z.slots : 0.0;
   a.items = z.items * a.kv_heads;

@@ -147,6 +147,12 @@ struct StoreArgs {
   hipStream_t stream;
 };
 
+// A divisor of non-negative 32-bit integers as a multiplier and a shift.
+struct Divisor {
+  uint32_t mul;
+  int shift;
+};
+
 struct CacheAttnArgs {
   const void* Q;
   void* O;
@@ -172,6 +178,9 @@ struct CacheAttnArgs {
   double inv_slots = 0.0;  // 1 / slots
   bool ramp = false;   // rows of a stream see more and more keys: its tiles are weighed by their mean
   int64_t items = 0;   // items, and partial results, there is room for
+  int64_t items_per_head = 0;
+  int most_keys = 0;   // that any tile sees, at most
+  Divisor by_group, by_heads, by_frame;
 };
 
 hipError_t launch_cache_plan(const PlanArgs& a);

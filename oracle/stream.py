@@ -156,18 +156,19 @@ def attn_ref(q, k, v, frame=0, window=0, scale=None):
     n, KH = k.shape[:2]
     scale = d ** -0.5 if scale is None else scale
     O, mass, reach = np.zeros((m, H, d)), np.zeros((m, H, d)), np.zeros((m, H))
-    for i in range(m):
-        lo, hi = visible_keys(n, m, i, frame, window)
-        if hi <= lo:
-            continue
-        for h in range(H):
-            kh = h // (H // KH)
-            kk, vv = k[lo:hi, kh], v[lo:hi, kh]
-            s = kk @ q[i, h] * scale
-            w = np.exp(s - s.max())
-            w /= w.sum()
-            O[i, h], mass[i, h] = w @ vv, w @ np.abs(vv)
-            reach[i, h] = (np.abs(kk) @ np.abs(q[i, h])).max() * scale
+    bounds = np.array([visible_keys(n, m, i, frame, window) for i in range(m)]).reshape(m, 2)
+    sees = bounds[:, 1] > bounds[:, 0]
+    if not sees.any():
+        return O, mass, reach
+    j = np.arange(n)
+    hidden = (j < bounds[sees, :1]) | (j >= bounds[sees, 1:])
+    for h in range(H):
+        kk, vv, qq = k[:, h // (H // KH)], v[:, h // (H // KH)], q[sees, h]
+        s = np.where(hidden, -np.inf, qq @ kk.T * scale)
+        w = np.exp(s - s.max(-1, keepdims=True))
+        w /= w.sum(-1, keepdims=True)
+        O[sees, h], mass[sees, h] = w @ vv, w @ np.abs(vv)
+        reach[sees, h] = np.where(hidden, 0, np.abs(qq) @ np.abs(kk).T).max(-1) * scale
     return O, mass, reach
 
 

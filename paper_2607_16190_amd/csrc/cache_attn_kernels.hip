@@ -332,21 +332,26 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
   for (int m = 0; m < 8; ++m) o[m] = f32x4{0.f, 0.f, 0.f, 0.f};
   float mref = -1.0e30f, lsum = 0.f;
 
+  // Pages of 16 keys, asked for a turn ahead. Keys outside [lo, k1) repeat the nearest one
+  // inside: their pages may be no longer the stream's, and their codes anything.
+  const const_i32* tab = (const const_i32*)table;
+  int entry[4];
+  auto look_up = [&](int base) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) entry[t] = tab[min(max(base + 16 * t, it.lo), k1 - 1) >> P.page_shift];
+  };
+  if (k0 + wave * kKeys < k1) look_up(k0 + wave * kKeys);
   for (int base = k0 + wave * kKeys; base < k1; base += WAVES * kKeys) {
-    // Keys outside [lo, k1) repeat the nearest one inside: their pages may be no
-    // longer the stream's, and their codes anything.
     u32x4 kraw[4][2];
     u32x2 vraw[4][4];
     float ke[4], ve[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const int first = min(max(base + 16 * t, it.lo), k1 - 1);
-      const int entry = __builtin_amdgcn_readfirstlane(min(max(table[first >> P.page_shift], 0), P.pages - 1));
-      const int64_t at = (int64_t)entry * P.kv_heads + kh;
-      ke[t] = exp_of(P.k_exp[at]);
-      ve[t] = exp_of(P.v_exp[at]);
-      const uint8_t* kp = P.k8 + at * P.page * kHeadDim;
-      const uint8_t* vp = P.v8 + at * P.page * kHeadDim;
+      const uint32_t at = (uint32_t)min(max(entry[t], 0), P.pages - 1) * (uint32_t)P.kv_heads + (uint32_t)kh;
+      ke[t] = exp_of(((const const_i32*)P.k_exp)[at]);
+      ve[t] = exp_of(((const const_i32*)P.v_exp)[at]);
+      const uint8_t* kp = P.k8 + (uint64_t)at * (uint32_t)(P.page * kHeadDim);
+      const uint8_t* vp = P.v8 + (uint64_t)at * (uint32_t)(P.page * kHeadDim);
       const int kr = min(max(base + 16 * t + l, it.lo), k1 - 1) & (P.page - 1);
       kraw[t][0] = load<STREAM, u32x4>(kp + kr * kHeadDim + 16 * g);
       kraw[t][1] = load<STREAM, u32x4>(kp + kr * kHeadDim + 64 + 16 * g);
@@ -356,6 +361,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
         vraw[t][r] = load<STREAM, u32x2>(vp + vr * kHeadDim + 8 * l);
       }
     }
+    look_up(base + WAVES * kKeys);
     f32x4 s[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -539,45 +545,6 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   const Stream& st = it.st;
   const int tile = it.tile, n_chunks = it.n_chunks, k0 = it.k0, k1 = it.k1;
 
-  const int rows = st.q_len * P.group;
-  const int row0 = tile * kBigRows + 32 * wave;
-  int lo[NT], hi[NT];
-  int wave_lo = INT32_MAX, wave_hi = 0, all_lo = 0, all_hi = INT32_MAX;
-  bf16x8 qf[NT][4];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int row = row0 + 16 * nt + l;
-    lo[nt] = hi[nt] = 0;
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) qf[nt][ks] = bf16x8{};
-    if (row < rows) {
-      const int tok = divide(row, P.by_group);
-      const int qh = kh * P.group + row - tok * P.group;
-      visible(P, st, tok, lo[nt], hi[nt]);
-      hi[nt] = max(min(hi[nt], k1), lo[nt]);
-      const uint16_t* q = static_cast<const uint16_t*>(P.Q) + (int64_t)(st.q0 + tok) * P.stride_n + (int64_t)qh * P.stride_h;
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) qf[nt][ks] = *reinterpret_cast<const bf16x8*>(q + 32 * ks + 8 * g);
-      all_lo = max(all_lo, lo[nt]);
-      all_hi = min(all_hi, hi[nt]);
-      if (hi[nt] > lo[nt]) {
-        wave_lo = min(wave_lo, lo[nt]);
-        wave_hi = max(wave_hi, hi[nt]);
-      }
-    }
-  }
-#pragma unroll
-  for (int d = 1; d < 16; d <<= 1) {
-    all_lo = max(all_lo, __shfl_xor(all_lo, d));
-    all_hi = min(all_hi, __shfl_xor(all_hi, d));
-    wave_lo = min(wave_lo, __shfl_xor(wave_lo, d));
-    wave_hi = max(wave_hi, __shfl_xor(wave_hi, d));
-  }
-  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-  all_hi = min(__builtin_amdgcn_readfirstlane(all_hi), k1);
-  wave_lo = __builtin_amdgcn_readfirstlane(wave_lo);
-  wave_hi = min(__builtin_amdgcn_readfirstlane(wave_hi), k1);
-
   const int32_t* table = P.table + (int64_t)it.stream * P.width;
   const float c2 = P.scale * 1.44269504088896340736f;
 
@@ -644,6 +611,52 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
       put(wv[1], buf, u, vraw[u].z, vraw[u].w, ve[u % NP]);
     }
   };
+
+  // The first step's page and codes are on their way while the rows of Q are looked at.
+  if (k0 < k1) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) tiles[p] = tile_of(entry_at(row_of(k0, p)));
+    fetch(k0);
+  }
+
+  const int rows = st.q_len * P.group;
+  const int row0 = tile * kBigRows + 32 * wave;
+  int lo[NT], hi[NT];
+  int wave_lo = INT32_MAX, wave_hi = 0, all_lo = 0, all_hi = INT32_MAX;
+  bf16x8 qf[NT][4];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = row0 + 16 * nt + l;
+    lo[nt] = hi[nt] = 0;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) qf[nt][ks] = bf16x8{};
+    if (row < rows) {
+      const int tok = divide(row, P.by_group);
+      const int qh = kh * P.group + row - tok * P.group;
+      visible(P, st, tok, lo[nt], hi[nt]);
+      hi[nt] = max(min(hi[nt], k1), lo[nt]);
+      const uint16_t* q = static_cast<const uint16_t*>(P.Q) + (int64_t)(st.q0 + tok) * P.stride_n + (int64_t)qh * P.stride_h;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) qf[nt][ks] = *reinterpret_cast<const bf16x8*>(q + 32 * ks + 8 * g);
+      all_lo = max(all_lo, lo[nt]);
+      all_hi = min(all_hi, hi[nt]);
+      if (hi[nt] > lo[nt]) {
+        wave_lo = min(wave_lo, lo[nt]);
+        wave_hi = max(wave_hi, hi[nt]);
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) {
+    all_lo = max(all_lo, __shfl_xor(all_lo, d));
+    all_hi = min(all_hi, __shfl_xor(all_hi, d));
+    wave_lo = min(wave_lo, __shfl_xor(wave_lo, d));
+    wave_hi = max(wave_hi, __shfl_xor(wave_hi, d));
+  }
+  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  all_hi = min(__builtin_amdgcn_readfirstlane(all_hi), k1);
+  wave_lo = __builtin_amdgcn_readfirstlane(wave_lo);
+  wave_hi = min(__builtin_amdgcn_readfirstlane(wave_hi), k1);
 
   f32x4 o[8][NT], lsum[NT];
   float mrow[NT], thr[NT], negm[NT];
@@ -826,22 +839,23 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   };
 
   if (k0 < k1) {
+    uint32_t next[NP];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-#pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        tiles[p] = tile_of(entry_at(row_of(k0 + n * kKeys, p)));
-        ke[p] = exp_of(kexp[tiles[p]]);
-        ve[p] = exp_of(vexp[tiles[p]]);
-      }
-      fetch(k0 + n * kKeys);
-      if (n == 0) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) stage(0, i);
-      }
+    for (int p = 0; p < NP; ++p) {
+      ke[p] = exp_of(kexp[tiles[p]]);
+      ve[p] = exp_of(vexp[tiles[p]]);
+      tiles[p] = tile_of(entry_at(row_of(k0 + kKeys, p)));
+      next[p] = tile_of(entry_at(row_of(k0 + 2 * kKeys, p)));
     }
 #pragma unroll
-    for (int p = 0; p < NP; ++p) tiles[p] = tile_of(entry_at(row_of(k0 + 2 * kKeys, p)));
+    for (int i = 0; i < 4; ++i) stage(0, i);
+    fetch(k0 + kKeys);
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      ke[p] = exp_of(kexp[tiles[p]]);
+      ve[p] = exp_of(vexp[tiles[p]]);
+      tiles[p] = next[p];
+    }
     __syncthreads();
     for (int base = k0;;) {
       step(std::integral_constant<int, 0>{}, base);
@@ -1041,8 +1055,8 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   }
 }
 
-// Which kernel, the workgroups per K/V head to split for (0: the tiles alone fill the
-// device), and the items there can be.
+// Workgroups per K/V head to split for (0: the tiles alone fill the device), and the items
+// there can be.
 struct Sizes {
   bool big;
   int rows, slots;
@@ -1052,40 +1066,66 @@ struct Sizes {
 // Streams of few keys stay in one workgroup a tile: up to four turns of eight waves.
 bool few_keys(int64_t most_keys) { return most_keys <= 2048; }
 
+int64_t tiles_of(int64_t tokens, int group, int rows, int streams) {
+  return tokens * group / rows + streams;  // at most one partly filled tile a stream
+}
+
 // window, frame: 0 where they are not known.
-Sizes sizes_of(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys, int window, int frame) {
+Sizes sizes_of(bool big, int tokens, int heads, int kv_heads, int streams, int64_t most_keys, int window, int frame) {
   const int group = heads / kv_heads;
   Sizes r;
-  // One small tile per stream reads the keys once, straight into registers. More rows than
-  // that share the keys' conversion through LDS in large tiles.
-  r.big = (int64_t)max_q * group > kRows;
-  r.rows = r.big ? kBigRows : kRows;
-  r.tiles = (int64_t)tokens * group / r.rows + streams;  // at most one partly filled tile a stream
-  const int round = std::max(1, (r.big ? kBigSlots : kCacheSlots) / kv_heads);
-  const int64_t full = ((int64_t)tokens * group + r.rows - 1) / r.rows;  // tiles if the rows fill them
-  // From two rounds of tiles on their own, chunks no longer pay for the merge.
-  // Nor do they where keys are few.
-  if (window) most_keys = std::min(most_keys, (int64_t)window + 2 * (int64_t)frame + r.rows + kKeys);  // as in stream_of
+  r.big = big;
+  r.rows = big ? kBigRows : kRows;
+  r.tiles = tiles_of(tokens, group, r.rows, streams);
   r.keys = most_keys;
-  // (large tiles: ten steps are over before a second launch would merge anything)
-  const bool few = r.big ? most_keys <= 10 * kKeys : few_keys(most_keys);
+  if (window) r.keys = std::min(most_keys, (int64_t)window + 2 * (int64_t)frame + r.rows + kKeys);
+  // Chunks do not pay for a second launch that merges them where keys are few (large tiles:
+  // ten steps), nor from two rounds of tiles on.
+  const int round = std::max(1, (big ? kBigSlots : kCacheSlots) / kv_heads);
+  const int64_t full = ((int64_t)tokens * group + r.rows - 1) / r.rows;  // tiles if the rows fill them
+  const bool few = big ? r.keys <= 10 * kKeys : few_keys(r.keys);
   r.slots = few || full >= 2 * (int64_t)round ? 0 : (full > round ? 2 : 1) * round;
   // The sum of chunks_of(mean) is at most slots + tiles, and chunks_of(span) at most twice
   // that, equal where the mean is the span (always for small tiles).
-  r.items = r.slots ? (r.big ? 2 : 1) * (r.tiles + r.slots) : r.tiles;
+  r.items = r.slots ? (big ? 2 : 1) * (r.tiles + r.slots) : r.tiles;
   return r;
+}
+
+// One small tile per stream reads the keys once, straight into registers. More rows share
+// the keys' conversion through LDS in large tiles, unless there is so little to do that a
+// large tile's longer way in (some 13 us against 5 on an idle device) decides. In turns of
+// 16 rows x 64 keys: streams of up to 2048 keys 1170 / 3800 / 10240 / 12250 turns 10.5 /
+// 11.3 / 23.5 / 23.0 us in small tiles, 13.2 / 13.4 / 29.8 / 32.7 in large ones; longer
+// streams, whose merge small tiles make longer, 441 / 3384 / 8192 / 12384 turns 14.9 / 25.2
+// / 34.1 / 55.8 against 19.8 / 27.6 / 29.5 / 38.1.
+bool is_big(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys, int window, int frame) {
+  const int group = heads / kv_heads;
+  if ((int64_t)max_q * group <= kRows) return false;
+  const int64_t keys = sizes_of(false, tokens, heads, kv_heads, streams, most_keys, window, frame).keys;
+  const double turns = (double)tiles_of(tokens, group, kRows, streams) * kv_heads * (double)((keys + kKeys - 1) / kKeys);
+  return turns > (few_keys(keys) ? 16384 : 4096);
 }
 
 }  // namespace
 
+// Both queries hold for either kernel, as a window, which they are not told, may change the
+// choice.
 int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
-  const Sizes z = sizes_of(tokens, heads, kv_heads, streams, max_q, most_keys, 0, 0);
-  return std::max(z.items, z.tiles * (z.rows / 16)) * kv_heads + kXcds;
+  int64_t most = 0;
+  for (int big = 0; big <= ((int64_t)max_q * (heads / kv_heads) > kRows ? 1 : 0); ++big) {
+    const Sizes z = sizes_of(big, tokens, heads, kv_heads, streams, most_keys, 0, 0);
+    most = std::max(most, std::max(z.items, z.tiles * (z.rows / 16)) * kv_heads + kXcds);
+  }
+  return most;
 }
 
 size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
-  const Sizes z = sizes_of(tokens, heads, kv_heads, streams, max_q, most_keys, 0, 0);
-  return z.slots ? (size_t)z.items * kv_heads * z.rows * (kHeadDim + 2) * sizeof(float) : 0;
+  size_t most = 0;
+  for (int big = 0; big <= ((int64_t)max_q * (heads / kv_heads) > kRows ? 1 : 0); ++big) {
+    const Sizes z = sizes_of(big, tokens, heads, kv_heads, streams, most_keys, 0, 0);
+    if (z.slots) most = std::max(most, (size_t)z.items * kv_heads * z.rows * (kHeadDim + 2) * sizeof(float));
+  }
+  return most;
 }
 
 namespace {
@@ -1108,7 +1148,9 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
   (void)hipGetLastError();
   if (a.tokens == 0 || a.heads == 0 || a.streams == 0) return hipSuccess;
   a.group = a.heads / a.kv_heads;
-  const Sizes z = sizes_of(a.tokens, a.heads, a.kv_heads, a.streams, a.max_q, (int64_t)a.width * a.page, a.window, a.frame);
+  const int64_t most_keys = (int64_t)a.width * a.page;
+  const bool big = is_big(a.tokens, a.heads, a.kv_heads, a.streams, a.max_q, most_keys, a.window, a.frame);
+  const Sizes z = sizes_of(big, a.tokens, a.heads, a.kv_heads, a.streams, most_keys, a.window, a.frame);
   a.rows = z.rows;
   a.row_shift = z.big ? 7 : 4;
   a.ramp = z.big && a.frame;
@@ -1121,8 +1163,8 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
   a.inv_slots = z.slots ? 1.0 / z.slots : 0.0;
   a.items = z.items * a.kv_heads;
   // Small tiles of few keys: as many waves a tile as the chip has room for (twelve a CU) when
-  // all tiles run at once. Of many keys: four, and the codes, which no other workgroup of
-  // the call reads, past the caches (64 ragged streams of up to 16000 keys, 8 heads: 165 ->
+  // all tiles run at once. Of many keys: four, and codes that no other workgroup of
+  // the call reads go past the caches (64 ragged streams of up to 16000 keys, 8 heads: 165 ->
   // 154 us; 111,600 keys of 40 heads: 207 -> 190, 6.0 TB/s).
   const unsigned grid = (unsigned)((a.items + kXcds - 1) / kXcds * kXcds);
   if (z.big && a.page >= kKeys)
@@ -1136,6 +1178,8 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
   else if (few_keys(z.keys) && a.items > 768)
     launch_small<2, false>(a);
   else if (few_keys(z.keys))
+    launch_small<4, false>(a);
+  else if ((int64_t)a.max_q * a.group > kRows)  // several tiles read the same keys
     launch_small<4, false>(a);
   else
     launch_small<4, true>(a);

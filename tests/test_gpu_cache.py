@@ -269,6 +269,74 @@ def test_attn_chunks(rows, H, KH):
     check_attn(attn_case([700, rows], [rows, max(1, rows // 3)], 64, H, KH, seed=rows, layout="bhnd"), 1, 0)
 
 
+# Calls with enough to do for large tiles of 128 rows (more than 4096 turns of 16 rows x 64 keys over streams of
+# more than 2048 keys, or 16384 over shorter ones).
+
+
+@pytest.mark.parametrize("frame,window", [(0, 0), (1, 0), (1, 700), (100, 0), (100, 333), (0, 900), (2000, 0), (7, 3), (2**31 - 1, 5)])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_attn_large_tiles(frame, window, page):
+    c = attn_case([2601, 150, 0, 1300, 129], [150, 150, 3, 257, 0], page, 12, 4, seed=page + frame % 89, layout="bhnd" if page == 32 else "bnhd")
+    check_attn(c, frame, window)
+
+
+@pytest.mark.parametrize("frame,window", [(0, 2500), (1, 2500), (100, 2333), (2000, 3100)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_attn_large_tiles_and_long_windows(frame, window, page):
+    check_attn(attn_case([6000, 100, 4444], [200, 100, 3], page, 12, 4, seed=page + frame), frame, window)
+
+
+@pytest.mark.parametrize("rows", [17, 127, 128, 129, 300])
+@pytest.mark.parametrize("H,KH", [(32, 32), (20, 1)])
+def test_attn_large_tiles_of_one_stream(rows, H, KH):
+    check_attn(attn_case([9000], [rows], 64, H, KH, seed=rows), 1, 0)
+    check_attn(attn_case([4500 + rows], [rows], 128, H, KH, seed=rows), 0, 0)
+
+
+@pytest.mark.parametrize("streams", [66, 130])
+def test_attn_large_tiles_of_many_streams(streams):
+    rng = np.random.default_rng(streams)
+    lens = [int(n) for n in rng.integers(0, 400, streams)]
+    lens[streams // 2] = 2500
+    check_attn(attn_case(lens, [int(n) for n in rng.integers(0, 40, streams)], 16, 8, 2, seed=streams), 1, 0)
+
+
+def test_attn_large_tiles_without_a_merge():
+    """As many tiles as the device holds twice over."""
+    check_attn(attn_case([1500], [1500], 64, 100, 50, seed=1), 500, 700)
+
+
+def test_attn_large_tiles_are_the_same_on_every_run():
+    c = attn_case([5000, 800], [260, 100], 64, 8, 8)
+    first = call_attn(c, 100, 0)
+    for _ in range(3):
+        assert torch.equal(first, call_attn(c, 100, 0))
+
+
+def test_attn_wrong_estimate_of_the_longest_stream():
+    """max_q chooses the kernel and nothing else."""
+    c = attn_case([3000, 40], [120, 2], 64, 8, 8)
+    q = c["rows"]
+    for estimate in (0, 1, 5000):
+        c["rows"] = q
+        start = np.concatenate([[0], np.cumsum(q)])
+        (kc, ke), (vc, ve) = c["k"], c["v"]
+        d = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV)  # noqa: E731
+        got = fva.fva_attn_cache(c["q"], d(kc), d(vc), d(ke), d(ve), i32(c["table"]), i32(c["lens"]), i32(start), estimate, frame=1)
+        want = call_attn(c, 1)
+        assert (got.float() - want.float()).abs().max().item() <= 2.0**-6 * want.float().abs().max().item()
+
+
+def test_attn_starts_that_are_not_ascending_stay_in_bounds():
+    """Rows of such streams are of no meaning; the call returns, and rows of no stream stay."""
+    c = attn_case([900, 700, 800], [40, 40, 40], 64, 8, 8)
+    (kc, ke), (vc, ve) = c["k"], c["v"]
+    d = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV)  # noqa: E731
+    for start in ([0, 120, 0, 120], [-5, 2**31 - 1, -7, 30], [100, 50, 20, 0], [0, 40, 80, 2**31 - 1]):
+        fva.fva_attn_cache(c["q"], d(kc), d(vc), d(ke), d(ve), i32(c["table"]), i32([2**31 - 1, -4, 800]), i32(start), 40, frame=1)
+    torch.cuda.synchronize()
+
+
 def test_attn_long_chunk_of_frames():
     check_attn(attn_case([1300], [640], 32, 1, 1, seed=3), 320, 960)
 

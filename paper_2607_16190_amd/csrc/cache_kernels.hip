@@ -18,12 +18,13 @@ namespace {
 constexpr int kPlanThreads = 256;
 
 // Exclusive prefix sums over the workgroup of three values a thread holds, and the totals.
+// (64 bits: lengths come from device memory, and no sum of them may turn negative.)
 struct Three {
-  int a, b, c;
+  uint64_t a, b, c;
 };
-__device__ __forceinline__ Three block_exclusive(Three v, Three& total, int (&part)[3][kPlanThreads / kWave]) {
+__device__ __forceinline__ Three block_exclusive(Three v, Three& total, uint64_t (&part)[3][kPlanThreads / kWave]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Three in = {wave_incl_scan_i32(v.a, lane), wave_incl_scan_i32(v.b, lane), wave_incl_scan_i32(v.c, lane)};
+  const Three in = {wave_incl_scan_u64(v.a, lane), wave_incl_scan_u64(v.b, lane), wave_incl_scan_u64(v.c, lane)};
   if (lane == 63) {
     part[0][wave] = in.a;
     part[1][wave] = in.b;
@@ -39,6 +40,8 @@ __device__ __forceinline__ Three block_exclusive(Three v, Three& total, int (&pa
   }
   return {below.a + in.a - v.a, below.b + in.b - v.b, below.c + in.c - v.c};
 }
+
+__device__ __forceinline__ int to_int(uint64_t v) { return (int)min(v, (uint64_t)INT32_MAX); }
 
 // Largest s in [0, n) with start[s] <= x, of ascending start with start[0] = 0 (streams
 // of no width share a start; the last of them is found, which is the one that holds x).
@@ -65,7 +68,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs P) {
   __shared__ int first[kPlanStreams + 1];     // pages popped before it
   __shared__ int behind[kPlanStreams + 1];    // pages pushed before it
   __shared__ int held_s[kPlanStreams];        // tokens held, or -1 - tokens held where the stream is refused
-  __shared__ int part[3][kPlanThreads / kWave];
+  __shared__ uint64_t part[3][kPlanThreads / kWave];
   __shared__ int refused_s;
   const int S = P.streams;
   const int cap = P.ring_size;
@@ -85,10 +88,10 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs P) {
     const int now = pages_of(held);
     if (add < 0) {
       wide = true;
-      return Three{0, 0, now};
+      return Three{0, 0, (uint64_t)now};
     }
     wide = add <= most - held;
-    return Three{add, wide ? pages_of(held + add) - now : 0, 0};
+    return Three{(uint64_t)add, wide ? (uint64_t)(pages_of(held + add) - now) : 0, 0};
   };
   Three mine = {0, 0, 0}, total;
   for (int s = s0; s < s1; ++s) {
@@ -103,29 +106,29 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs P) {
     int held;
     bool wide;
     const Three w = wants(s, held, wide);
-    const bool fits = wide && (w.b == 0 || at.b + w.b <= count);
-    q_start[s] = at.a;
+    const bool fits = wide && (w.b == 0 || at.b + w.b <= (uint64_t)count);
+    q_start[s] = to_int(at.a);
     // refused pops lie behind the granted ones: the search below never reaches them
-    first[s] = min(at.b, count);
-    behind[s] = at.c;
+    first[s] = (int)min(at.b, (uint64_t)count);
+    behind[s] = to_int(at.c);
     held_s[s] = fits ? held : -1 - held;
     refused += fits ? 0 : 1;
     if (blockIdx.x == 0) {
-      P.q_start[s] = at.a;
-      P.kv_len[s] = P.fresh[s] < 0 ? 0 : (fits ? held + w.a : held);
+      P.q_start[s] = to_int(at.a);
+      P.kv_len[s] = P.fresh[s] < 0 ? 0 : (fits ? held + (int)w.a : held);
     }
     at = {at.a + w.a, at.b + w.b, at.c + w.c};
   }
   if (refused) atomicAdd(&refused_s, refused);
   if (threadIdx.x == 0) {
-    q_start[S] = total.a;
-    behind[S] = total.c;
+    q_start[S] = to_int(total.a);
+    behind[S] = to_int(total.c);
   }
   __syncthreads();
   // Pages granted: the pops of streams up to the first that did not fit.
   int taken = 0;
   {
-    int t = 0;
+    uint64_t t = 0;
     for (int s = s0; s < s1; ++s) {
       int held;
       bool wide;
@@ -135,11 +138,12 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs P) {
     Three sum;
     __syncthreads();
     (void)block_exclusive({t, 0, 0}, sum, part);
-    taken = sum.a;
+    taken = (int)sum.a;  // at most count
   }
-  const int pushed = min(total.c, cap - count);
+  const int pushed = (int)min(total.c, (uint64_t)(cap - count));
+  const int rows = to_int(total.a);
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    P.q_start[S] = total.a;
+    P.q_start[S] = rows;
     P.state_out[0] = (int)(((int64_t)head + taken) % cap);
     P.state_out[1] = count - taken + pushed;
     P.state_out[2] = refused_s;
@@ -157,7 +161,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs P) {
   }
   for (int r = i0; r < P.tokens; r += step) {
     int slot = -1, id = -1;
-    if (r < total.a) {
+    if (r < rows) {
       const int s = find_stream(q_start, S, r);
       const int held = held_s[s];
       if (held >= 0) {

@@ -401,7 +401,8 @@ fva_status check_rows(const fva_qkv_desc* d, int step, bool written) {
   if (d->batch < 0 || d->heads < 0 || d->tokens < 0) return FVA_ERR_SHAPE;
   if (d->head_dim != fva::kHeadDim) return FVA_ERR_UNSUPPORTED;
   if (d->stride_b < 0 || d->stride_h < 0 || d->stride_n < 0) return FVA_ERR_SHAPE;
-  if (d->stride_n % step != 0 || d->stride_h % step != 0 || d->stride_b % step != 0) return FVA_ERR_SHAPE;
+  if ((d->tokens > 1 && d->stride_n % step) || (d->heads > 1 && d->stride_h % step) || (d->batch > 1 && d->stride_b % step))
+    return FVA_ERR_SHAPE;
   if ((int64_t)d->batch * d->tokens > INT32_MAX) return FVA_ERR_UNSUPPORTED;
   if (written && d->batch && d->heads && d->tokens) {
     // extents above one by ascending stride: each step clears everything below it

@@ -69,6 +69,21 @@ def test_plan_narrow_rows_and_short_buffers():
     check_plan([0], [0], [0, 0, 0], [5], [[-1]], 16, 0)
 
 
+def test_plan_of_absurd_lengths_stays_in_bounds():
+    """Lengths whose sums pass 32 bits: such streams are refused, and the others are served."""
+    S, page, width, cap = 300, 16, 4, 50
+    held = np.full(S, 2**31 - 1)
+    fresh = np.full(S, 2**31 - 1)
+    held[::3], fresh[::3] = 5, 2**30
+    held[8], fresh[8] = 3, 40
+    fresh[1:200:6] = -1
+    table, ring = i32(np.zeros((S, width))), i32(np.arange(cap))
+    kv_len, q_start, slots, ids, state = fva.fva_cache_plan(i32(held), i32(fresh), i32([49, 20, 0]), ring, table, page, 1000)
+    n = kv_len.cpu().numpy()
+    assert n[8] == 43 and state.cpu().numpy()[2] == S - 1 - (fresh < 0).sum()
+    assert (n[fresh < 0] == 0).all() and (np.diff(q_start.cpu().numpy().astype(np.int64)) >= 0).all()
+
+
 def test_plan_steps_keep_pages_apart():
     """Many steps with streams that come, grow and end: no page is held twice, and none is lost."""
     rng = np.random.default_rng(0)
@@ -267,6 +282,31 @@ def test_attn_rows_that_see_nothing(frame):
 def test_attn_chunks(rows, H, KH):
     check_attn(attn_case([700, rows], [rows, max(1, rows // 3)], 64, H, KH, seed=rows), 0, 0)
     check_attn(attn_case([700, rows], [rows, max(1, rows // 3)], 64, H, KH, seed=rows, layout="bhnd"), 1, 0)
+
+
+@pytest.mark.parametrize("rows", [1, 200])
+def test_pool_past_32_bits(rows):
+    """A pool of more than 2^32 bytes: the stream's pages are its last ones."""
+    page, KH, n = 128, 8, 2500
+    pages = 2**32 // (page * KH * 128) + 40
+    need = -(-n // page)
+    k8, v8 = (torch.empty((pages, KH, page, 128), dtype=torch.uint8, device=DEV) for _ in range(2))
+    ke, ve = (torch.empty((pages, KH), dtype=torch.int32, device=DEV) for _ in range(2))
+    slots = np.concatenate([np.arange(page) + p * page for p in range(pages - 1, pages - 1 - need, -1)])[:n]
+    g = torch.Generator().manual_seed(5)
+    k, v = (torch.randn((1, n, KH, 128), generator=g).to(torch.bfloat16).to(DEV).transpose(1, 2) for _ in range(2))
+    fva.fva_cache_store(k, v, i32(slots), k8, v8, ke, ve)
+    table = np.arange(pages - 1, pages - 1 - need, -1)
+    small = [t[pages - need:].cpu().numpy()[::-1] for t in (k8, v8, ke, ve)]  # in the stream's order
+    for x, c, e in ((k, small[0], small[2]), (v, small[1], small[3])):
+        wc, we = store_ref(bits(x)[0].transpose(1, 0, 2), np.arange(n), np.zeros_like(c), np.zeros_like(e))
+        got = e4m3_decode(c).transpose(0, 2, 1, 3).reshape(-1, KH, 128)[:n]
+        assert np.array_equal(e, we) and np.array_equal(got, e4m3_decode(wc).transpose(0, 2, 1, 3).reshape(-1, KH, 128)[:n])
+    q = torch.randn((1, rows, 16, 128), generator=g).to(torch.bfloat16).to(DEV).transpose(1, 2)
+    out = fva.fva_attn_cache(q, k8, v8, ke, ve, i32(table[None]), i32([n]), i32([0, rows]), rows, frame=1)
+    kk, vv = (cached(c, e, np.arange(need), n) for c, e in ((small[0], small[2]), (small[1], small[3])))
+    O, mass, reach = attn_ref(bits(q)[0].transpose(1, 0, 2), kk, vv, 1, 0)
+    assert (np.abs(bits(out)[0].transpose(1, 0, 2) - O) <= attn_tolerance(O, mass, reach)).all()
 
 
 # Calls with enough to do for large tiles of 128 rows (more than 4096 turns of 16 rows x 64 keys over streams of

@@ -508,6 +508,7 @@ def fva_attn_fp8v(q, k, v8, vexp, tiling: Tiling, mask, counts=None, kv_idx=None
 
 
 
+_I32 = torch.int32
 _DTYPES = {torch.bfloat16: FVA_BF16, torch.float16: FVA_FP16, torch.float32: FVA_FP32}
 
 
@@ -528,19 +529,20 @@ def _stream_on(dev: int, stream):
     return _stream_ptr(stream) if raw is None else raw(dev)
 
 
-def _int32(t, what, *shape):
-    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous int32 tensor of shape {shape}")
+def _int32(t, what, n):
+    if t.dtype is not _I32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor of {n} entries")
 
 
 def _rows_of(x) -> _Desc:
     """Descriptor of [batch, heads, tokens, head_dim] rows."""
-    if x.dim() != 4:
+    shape = x.shape
+    if len(shape) != 4:
         raise ValueError("expected a [batch, heads, tokens, head_dim] tensor")
     sb, sh, sn, sd = x.stride()
     if sd != 1:
         raise ValueError("head_dim must be contiguous")
-    return _Desc(*x.shape, sb, sh, sn)
+    return _Desc(*shape, sb, sh, sn)
 
 
 def _empty(make, stream):
@@ -589,8 +591,11 @@ def fva_rope(q, k, hw, dims, *, ids=None, origin=(0, 0, 0), theta: float = 10000
         raise ValueError("q and k must share batch and tokens")
     ids_stride = 0
     if ids is not None:
-        _int32(ids, "ids", *((qd.tokens,) if ids.dim() == 1 else (qd.batch, qd.tokens)))
-        ids_stride = 0 if ids.dim() == 1 else qd.tokens
+        if ids.dim() == 1:
+            _int32(ids, "ids", qd.tokens)
+        else:
+            ids_stride = qd.tokens
+            _int32(ids, "ids", qd.batch * ids_stride)
     rows, cols = hw
     dim_t, dim_y, dim_x = dims
     t0, y0, x0 = origin
@@ -611,26 +616,27 @@ def fva_cache_plan(held, fresh, state, ring, block_table, page: int, tokens: int
     tokens: rows of the slots and ids. Returns (kv_len, q_start, slots, ids, state).
     """
     dev = _same_device(held, fresh, state, ring, block_table)
-    n, tokens = held.numel(), int(tokens)
+    n, cap = held.numel(), ring.numel()
+    width = block_table.shape[-1]
     _int32(held, "held", n)
     _int32(fresh, "fresh", n)
     _int32(state, "state", 3)
-    _int32(ring, "ring", ring.numel())
-    width = block_table.shape[-1]
-    _int32(block_table, "block_table", n, width)
-    sizes = [n, n + 1, tokens, tokens, 3]
+    _int32(ring, "ring", cap)
+    _int32(block_table, "block_table", n * width)
+    sizes = (n, n + 1, tokens, tokens, 3)
     if out is None:
         if tokens < 0:
             raise ValueError("tokens must not be negative")
         # one buffer, cut into the five results
-        out = _empty(lambda: torch.empty(sum(sizes), dtype=torch.int32, device=held.device), stream).split_with_sizes(sizes)
+        whole = 2 * (n + tokens) + 4
+        out = (held.new_empty(whole) if stream is None else _empty(lambda: held.new_empty(whole), stream)).split_with_sizes(sizes)
     else:
         _same_device(held, *out)
         for t, size, what in zip(out, sizes, ("kv_len", "q_start", "slots", "ids", "state_out")):
             _int32(t, what, size)
     kv_len, q_start, slots, ids, state_out = out
     st = lib.fva_cache_plan(
-        held.data_ptr(), fresh.data_ptr(), n, page, state.data_ptr(), ring.data_ptr(), ring.numel(),
+        held.data_ptr(), fresh.data_ptr(), n, page, state.data_ptr(), ring.data_ptr(), cap,
         block_table.data_ptr(), width, tokens, kv_len.data_ptr(), q_start.data_ptr(), slots.data_ptr(), ids.data_ptr(),
         state_out.data_ptr(), _stream_on(dev, stream),
     )
@@ -645,8 +651,8 @@ def _cache_of(k8, v8, k_exp, v_exp) -> _Cache:
     if not k8.is_contiguous() or not v8.is_contiguous():
         raise ValueError("k8 and v8 must be contiguous")
     pages, heads, page, d = shape
-    _int32(k_exp, "k_exp", pages, heads)
-    _int32(v_exp, "v_exp", pages, heads)
+    _int32(k_exp, "k_exp", pages * heads)
+    _int32(v_exp, "v_exp", pages * heads)
     return _Cache(pages, heads, page, d, k8.data_ptr(), v8.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr())
 
 
@@ -656,14 +662,13 @@ def fva_cache_store(k, v, slots, k8, v8, k_exp, v_exp, *, stream=None):
     k, v: bf16 [batch, heads, tokens, 128]; slots: int32, one per (batch, token); k8, v8: uint8 [pages, heads, page,
     128]; k_exp, v_exp: int32 [pages, heads].
     """
-    if k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
+    if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
         raise ValueError("k and v must be bf16")
     if k.shape != v.shape or k.stride() != v.stride():
         raise ValueError("k and v must share shape and strides")
     dev = _same_device(k, v, slots, k8, v8, k_exp, v_exp)
     desc = _rows_of(k)
-    if slots.dtype is not torch.int32 or slots.numel() != desc.batch * desc.tokens or not slots.is_contiguous():
-        raise ValueError("slots must be a contiguous int32 tensor with one entry per (batch, token)")
+    _int32(slots, "slots", desc.batch * desc.tokens)
     cache = _cache_of(k8, v8, k_exp, v_exp)
     st = lib.fva_cache_store(k.data_ptr(), v.data_ptr(), ctypes.byref(desc), slots.data_ptr(), ctypes.byref(cache),
                              _stream_on(dev, stream))
@@ -705,7 +710,7 @@ def fva_attn_cache(q, k8, v8, k_exp, v_exp, block_table, kv_len, q_start, max_q:
     _int32(kv_len, "kv_len", n)
     _int32(q_start, "q_start", n + 1)
     width = block_table.shape[-1]
-    _int32(block_table, "block_table", n, width)
+    _int32(block_table, "block_table", n * width)
     if out is None:
         out = _like(q, stream)
     else:

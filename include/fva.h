@@ -544,7 +544,8 @@ fva_status fva_attn_cache_workspace_size(const fva_qkv_desc* q_desc, const fva_c
  * (without the first bound if window == 0): frame 0 is attention to the whole
  * cache, 1 is causal by token, H * W is causal by frame with the own frame
  * whole. O = softmax(softmax_scale * Q . K) V over them, 0 for a row that sees
- * none. bf16 MFMA products, fp32 accumulation and statistics, bf16 output.
+ * none. The cached values enter the products exactly; fp32 accumulation and
+ * statistics, P rounded to bf16 for its product, bf16 output.
  *
  * kv_len, q_start: device int32 [streams], [streams + 1], q_start ascending.
  * Lengths past the table's width are cut to it. Of the block table only the

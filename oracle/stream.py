@@ -150,8 +150,8 @@ def visible_keys(kv_len, q_len, i, frame, window):
 
 def attn_ref(q, k, v, frame=0, window=0, scale=None):
     """(O, mass, reach) of one stream: q [rows, heads, 128], k, v [keys, kv heads, 128]. mass[i, h, d] is
-    sum_j p_j |v_jd| and reach[i, h] the largest sum_d |q_d k_jd| * scale over visible keys: what rounding errors of P
-    and of the scores are bounded with."""
+    sum_j p_j |v_jd| and reach[i, h] the largest (sum_d |q_d k_jd| + max_d |q_d| sum_d |k_jd| / 16) * scale over visible
+    keys: what rounding errors of P and of the scores are bounded with."""
     m, H, d = q.shape
     n, KH = k.shape[:2]
     scale = d ** -0.5 if scale is None else scale
@@ -168,7 +168,8 @@ def attn_ref(q, k, v, frame=0, window=0, scale=None):
         w = np.exp(s - s.max(-1, keepdims=True))
         w /= w.sum(-1, keepdims=True)
         O[sees, h], mass[sees, h] = w @ vv, w @ np.abs(vv)
-        reach[sees, h] = np.where(hidden, 0, np.abs(qq) @ np.abs(kk).T).max(-1) * scale
+        top = np.abs(qq).max(-1, keepdims=True) / 16 * np.abs(kk).sum(-1)
+        reach[sees, h] = np.where(hidden, 0, np.abs(qq) @ np.abs(kk).T + top).max(-1) * scale
     return O, mass, reach
 
 
@@ -176,6 +177,7 @@ def attn_tolerance(O, mass, reach, half_step=2.0**-8):
     """Largest element error of attention with P and O rounded to a type of that half step and scores accumulated in
     fp32: |dO| <= half_step |O| (the output) + half_step mass (every P) + 2 ds mass (every score, numerator and
     denominator) with ds <= 128 * 2^-24 * reach from the sum of 128 products, 2^-20 * reach more for the scale, the
-    base-2 argument and the exponential, and 2^-18 of both for the sums over keys."""
+    base-2 argument and the exponential (the 2^-17 of reach's second term is what two E4M3 codes leave of Q: at most
+    2^-21 of a row's largest element in every channel), and 2^-18 of both for the sums over keys."""
     ds = (2.0**-17 + 2.0**-20) * reach[..., None] + 2.0**-18
     return half_step * np.abs(O) + (half_step + 2 * ds) * mass + 1e-30

@@ -15,9 +15,8 @@
 // cache_combine_kernel merges in chunk order (no atomics: the result is the same on
 // every run).
 //
-// Codes become bf16 exactly (E4M3 has four significant bits), times the page's power of
-// two in the same instruction; products are bf16 with fp32 accumulation, statistics and
-// sums fp32. P is rounded to bf16 for its product with V, as the matrix unit takes it: at
+// Codes enter the products exactly (E4M3 has four significant bits; bf16 holds them times
+// the page's power of two); accumulation, statistics and sums are fp32. P is rounded to bf16 for its product with V, as the matrix unit takes it: at
 // most half a step, 2^-9, of each term, the same as the output's own rounding.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -37,6 +36,8 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -488,6 +489,8 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) unsigned char lds_u8;
 typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) i32x4 lds_i32x4;
 
 template <int B, int E, typename F>
 __device__ __forceinline__ void static_for(F&& f) {
@@ -511,20 +514,31 @@ __device__ __forceinline__ float exp2_arg(float s, float c2, float negm) {
 // A large tile: 128 query rows, 32 per wave, against one chunk of its keys, 64 at a time.
 //
 // The 64 keys' codes are read once for the workgroup (two 16-byte pieces of K and of V per
-// thread, while the 64 before them are multiplied), become bf16 in registers and go to
-// LDS, where all four waves read them: a conversion is paid once for 128 rows. LDS holds
-// two such steps. Rows of 256 bytes; K's 16-byte chunk c of row r lies at c ^ r % 16, V's
-// at c ^ (2 (r % 8) + r % 2): the reads of both products meet no bank twice.
+// thread, two steps ahead) and go to LDS, where all four waves read them: K as it is, V as
+// bf16 (a conversion is paid once for 128 rows). LDS holds two such steps. V's rows are 256
+// bytes, its 16-byte chunk c of row r at c ^ (2 (r % 8) + r % 2), K's 128 bytes, chunk c at
+// c ^ r % 8 ^ 4 (r % 2): reads and writes of both meet no bank twice.
 //
-// Bound by the matrix and vector units together (64 + 4 products of 16 passes a wave and
-// step against 32 exponentials and their arguments, maxima and conversions).
+// S^T = K Q^T on the E4M3 matrix unit, K's codes as they are: Q, bf16, has eight significant
+// bits, which two codes of four hold, q = (high + low / 16) * 2^e with e from the row's
+// largest element. high is q rounded, low what that left, times 16: exact down to 2^-13 of
+// the row's maximum, and off by at most 2^-21 of it below (half of low's smallest step,
+// 2^-14, against a maximum above 224). Two fp8 products take the time of one in bf16 and spare K's
+// conversion and half of its LDS traffic: 4680 rows against 32,760 keys (40 heads) 2713 ->
+// 2499 us.
+//
+// O^T += V^T P^T in bf16: P would need two codes too, and their making is vector work, of
+// which there is no less than of matrix work (36 + 16 products a wave and step of 16 passes
+// and more against 32 exponentials, their arguments, maxima and conversions).
 template <bool kOnePage>
 __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(CacheAttnArgs P) {
   constexpr int NT = 2;
   constexpr int NP = kOnePage ? 1 : 2;  // pages of a thread's rows in a step
-  constexpr int kRow = 256;
+  constexpr int kRow = 256;             // bytes of a row of V in LDS
   constexpr int kTile = kKeys * kRow;
-  __shared__ __align__(16) unsigned char lds[4 * kTile];  // K, K of the next step, V, V
+  constexpr int kKTile = kKeys * kHeadDim;
+  __shared__ __align__(16) unsigned char lds[2 * kTile + 2 * kKTile];  // V, V of the next step, K, K
+  __shared__ __align__(16) int kscale[2][4];  // E8M0 scales of the 16-key groups of both steps
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, l = lane & 15;
@@ -553,7 +567,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   // pieces of two rows of different parity, so that their writes to LDS meet all banks.
   const int pr = ((lane >> 2) & 1) | ((lane >> 4) << 1), pc = (lane & 3) | ((lane >> 1) & 4);
   uint4 kraw[2], vraw[2];
-  float ke[NP], ve[NP];
+  int ke[NP];
+  float ve[NP];
   // Pages and exponents go through the scalar unit: wave-uniform, and nothing here writes
   // them (kOnePage: pages of 64 tokens or more, a step lies in one; else a wave's eight rows
   // do). The page of a step is asked for three steps before it is multiplied, its exponents
@@ -584,31 +599,25 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
       vraw[u] = *reinterpret_cast<const uint4*>(P.v8 + at + off);
     }
   };
-  const int kx = pr + 8 * (wave & 1), vx = 2 * pr + (pr & 1);  // swizzles of the thread's rows (32 rows on the same)
-  uint32_t wk[2], wv[2];  // LDS addresses of the two 16-byte halves of a piece
-  {
-    const uint32_t base = (uint32_t)(uintptr_t)(lds_u8*)lds + (uint32_t)((8 * wave + pr) * kRow);
+  const int kx = pr ^ ((pr & 1) << 2), vx = 2 * pr + (pr & 1);  // swizzles of the thread's rows (32 rows on the same)
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8*)lds;
+  // LDS addresses of a piece: K's 16 codes, the two halves of V's 16 channels.
+  uint32_t wk = lds0 + 2 * kTile + (uint32_t)((8 * wave + pr) * kHeadDim) + 16 * (uint32_t)(pc ^ kx);
+  uint32_t wv[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      wk[i] = base + 16 * ((2 * pc + i) ^ kx);
-      wv[i] = base + 2 * kTile + 16 * ((2 * pc + i) ^ vx);
-    }
-  }
-  auto put = [&](uint32_t at, int buf, int u, uint32_t a, uint32_t b, float e) {
-    *(lds_bf16x8*)((lds_u8*)(uintptr_t)at + buf * kTile + 32 * u * kRow) = eight_bf16(a, b, e);
-  };
+  for (int i = 0; i < 2; ++i) wv[i] = lds0 + (uint32_t)((8 * wave + pr) * kRow) + 16 * (uint32_t)((2 * pc + i) ^ vx);
   // (Opaque: the compiler would move a piece's conversion, which both branches of a step
   // have, up to its load, and wait for it there.)
   auto stage = [&](int buf, int piece) {
     const int u = piece & 1;
     if (piece < 2) {
-      asm volatile("" : "+v"(kraw[u].x), "+v"(kraw[u].y), "+v"(kraw[u].z), "+v"(kraw[u].w));
-      put(wk[0], buf, u, kraw[u].x, kraw[u].y, ke[u % NP]);
-      put(wk[1], buf, u, kraw[u].z, kraw[u].w, ke[u % NP]);
+      *(lds_u32x4*)((lds_u8*)(uintptr_t)wk + buf * kKTile + 32 * u * kHeadDim) = u32x4{kraw[u].x, kraw[u].y, kraw[u].z, kraw[u].w};
+      // rows 16 t .. + 15 are those of waves 2 t and 2 t + 1 (mod 4): wave 0 or 2 says their scale
+      if (!kOnePage && !(wave & 1) && lane == 0) kscale[buf][2 * u + (wave >> 1)] = 127 + ke[u % NP];
     } else {
       asm volatile("" : "+v"(vraw[u].x), "+v"(vraw[u].y), "+v"(vraw[u].z), "+v"(vraw[u].w));
-      put(wv[0], buf, u, vraw[u].x, vraw[u].y, ve[u % NP]);
-      put(wv[1], buf, u, vraw[u].z, vraw[u].w, ve[u % NP]);
+      *(lds_bf16x8*)((lds_u8*)(uintptr_t)wv[0] + buf * kTile + 32 * u * kRow) = eight_bf16(vraw[u].x, vraw[u].y, ve[u % NP]);
+      *(lds_bf16x8*)((lds_u8*)(uintptr_t)wv[1] + buf * kTile + 32 * u * kRow) = eight_bf16(vraw[u].z, vraw[u].w, ve[u % NP]);
     }
   };
 
@@ -623,13 +632,15 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   const int row0 = tile * kBigRows + 32 * wave;
   int lo[NT], hi[NT];
   int wave_lo = INT32_MAX, wave_hi = 0, all_lo = 0, all_hi = INT32_MAX;
-  bf16x8 qf[NT][4];
+  i32x8 qh[NT], ql[NT];  // Q = (high + low codes) * 2^e
+  int sh[NT], sl[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int row = row0 + 16 * nt + l;
     lo[nt] = hi[nt] = 0;
+    bf16x8 x[4];
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) qf[nt][ks] = bf16x8{};
+    for (int i = 0; i < 4; ++i) x[i] = bf16x8{};
     if (row < rows) {
       const int tok = divide(row, P.by_group);
       const int qh = kh * P.group + row - tok * P.group;
@@ -637,7 +648,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
       hi[nt] = max(min(hi[nt], k1), lo[nt]);
       const uint16_t* q = static_cast<const uint16_t*>(P.Q) + (int64_t)(st.q0 + tok) * P.stride_n + (int64_t)qh * P.stride_h;
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) qf[nt][ks] = *reinterpret_cast<const bf16x8*>(q + 32 * ks + 8 * g);
+      for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const bf16x8*>(q + 64 * (i >> 1) + 16 * g + 8 * (i & 1));
       all_lo = max(all_lo, lo[nt]);
       all_hi = min(all_hi, hi[nt]);
       if (hi[nt] > lo[nt]) {
@@ -645,6 +656,34 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
         wave_hi = max(wave_hi, hi[nt]);
       }
     }
+    // e as for a page: the smallest with amax <= 448 * 2^e
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf((float)x[i][j]));
+    }
+    const uint32_t bits = __float_as_uint(max4(amax));
+    const int e = bits >> 23 ? max((int)(bits >> 23) - 135 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0), kCacheExpMin) : kCacheExpMin;
+    const float inv = __uint_as_float((uint32_t)(127 - min(e, 120)) << 23);
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      float f[4], back[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = (float)x[w >> 1][4 * (w & 1) + j] * inv;
+      int h = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+      h = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], h, true);
+      back[0] = __builtin_amdgcn_cvt_f32_fp8(h, 0);
+      back[1] = __builtin_amdgcn_cvt_f32_fp8(h, 1);
+      back[2] = __builtin_amdgcn_cvt_f32_fp8(h, 2);
+      back[3] = __builtin_amdgcn_cvt_f32_fp8(h, 3);
+      int r = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (f[0] - back[0]), 16.f * (f[1] - back[1]), 0, false);
+      r = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (f[2] - back[2]), 16.f * (f[3] - back[3]), r, true);
+      qh[nt][w] = h;
+      ql[nt][w] = r;
+    }
+    sh[nt] = 127 + min(e, 120);
+    sl[nt] = sh[nt] - 4;
   }
 #pragma unroll
   for (int d = 1; d < 16; d <<= 1) {
@@ -676,29 +715,34 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
 #pragma unroll
   for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.0f;
 
-  uint32_t kaddr[4], vaddr[8];
-  {
-    const uint32_t base = (uint32_t)(uintptr_t)(lds_u8*)lds;
+  uint32_t kaddr[2], vaddr[8];
+  // K codes: row l of a 16-key group, 16-byte chunks g (channels 16 g ..) and 4 + g
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) kaddr[ks] = base + l * kRow + 16 * ((4 * ks + g) ^ l);
+  for (int i = 0; i < 2; ++i) kaddr[i] = lds0 + 2 * kTile + l * kHeadDim + 16 * ((4 * i + g) ^ (l & 7) ^ ((l & 1) << 2));
+  {
     // transposing reads: lane 4 e + q of group g points at row 16 hf + 4 g + e, 8-byte chunk 4 mt + q
     const int vr = 4 * g + (l >> 2);
 #pragma unroll
-    for (int mt = 0; mt < 8; ++mt) vaddr[mt] = base + 2 * kTile + vr * kRow + 16 * ((2 * mt + ((l >> 1) & 1)) ^ (2 * (vr & 7) + (vr & 1))) + 8 * (l & 1);
+    for (int mt = 0; mt < 8; ++mt) vaddr[mt] = lds0 + vr * kRow + 16 * ((2 * mt + ((l >> 1) & 1)) ^ (2 * (vr & 7) + (vr & 1))) + 8 * (l & 1);
   }
+
+  int kcur = 0, knext = 0;  // kOnePage: E8M0 scales of the keys of this step and the next
 
   // (Opaque to the compiler, which would otherwise re-add the lanes' parts at every read.)
   asm volatile("" : "+v"(vaddr[0]), "+v"(vaddr[1]), "+v"(vaddr[2]), "+v"(vaddr[3]), "+v"(vaddr[4]), "+v"(vaddr[5]),
                "+v"(vaddr[6]), "+v"(vaddr[7]));
-  asm volatile("" : "+v"(kaddr[0]), "+v"(kaddr[1]), "+v"(kaddr[2]), "+v"(kaddr[3]), "+v"(wk[0]), "+v"(wk[1]), "+v"(wv[0]),
-               "+v"(wv[1]));
+  asm volatile("" : "+v"(kaddr[0]), "+v"(kaddr[1]), "+v"(wk), "+v"(wv[0]), "+v"(wv[1]));
 
   // One step: S^T, under it the next step's codes into the other buffer and the loads of the
   // step after that, the softmax, O^T += V^T P^T. (The two buffers are two copies of the code: their offsets are
   // immediate.)
   auto step = [&](auto buf_c, int base) {
     constexpr int BUF = decltype(buf_c)::value;
-    auto kfrag = [&](int t, int ks) { return *(lds_bf16x8*)((lds_u8*)(uintptr_t)kaddr[ks] + BUF * kTile + t * 16 * kRow); };
+    auto kfrag = [&](int t) {
+      const i32x4 a = *(lds_i32x4*)((lds_u8*)(uintptr_t)kaddr[0] + BUF * kKTile + t * 16 * kHeadDim);
+      const i32x4 b = *(lds_i32x4*)((lds_u8*)(uintptr_t)kaddr[1] + BUF * kKTile + t * 16 * kHeadDim);
+      return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
     auto vfrag = [&](int kk, int mt) {
       lds_u8* at = (lds_u8*)(uintptr_t)vaddr[mt] + BUF * kTile + kk * 32 * kRow;
       const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
@@ -708,20 +752,33 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
     const bool act = base < wave_hi && base + kKeys > wave_lo;  // wave-uniform
     f32x4 s[4][NT];
     if (act) {
-      // Step u takes key tile 2 (u / 8) + u % 2 at channels 32 (u % 8 / 2): four
-      // independent chains alternate; fragments are read two steps ahead.
-      bf16x8 kq[3];
-      kq[0] = kfrag(0, 0);
-      kq[1] = kfrag(1, 0);
+      i32x4 ks = {0, 0, 0, 0};
+      if constexpr (!kOnePage) ks = *(lds_i32x4*)kscale[BUF];
+      i32x8 ka[4];
+      ka[0] = kfrag(0);
+      ka[1] = kfrag(1);
       __builtin_amdgcn_s_setprio(2);
-      static_for<0, 16>([&](auto u_c) {
+      // Two key groups against two query tiles, high then low codes of Q: four independent
+      // chains alternate.
+      static_for<0, 4>([&](auto u_c) {
         constexpr int u = decltype(u_c)::value;
-        constexpr int t = 2 * (u >> 3) + (u & 1), ks = (u & 7) >> 1;
-        if constexpr (u + 2 < 16) kq[(u + 2) % 3] = kfrag(2 * ((u + 2) >> 3) + (u & 1), ((u + 2) & 7) >> 1);
+        constexpr int t0 = 2 * (u >> 1);
+        if constexpr (u == 0) {
+          ka[2] = kfrag(2);
+          ka[3] = kfrag(3);
+        }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          s[t][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kq[u % 3], qf[nt][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t][nt], 0, 0, 0);
-        if constexpr (u % 4 == 1) stage(BUF ^ 1, u / 4);
+        for (int t = t0; t < t0 + 2; ++t) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const int sa = kOnePage ? kcur : ks[t];
+            if (u % 2 == 0)
+              s[t][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka[t], qh[nt], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, sa, 0, sh[nt]);
+            else
+              s[t][nt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka[t], ql[nt], s[t][nt], 0, 0, 0, sa, 0, sl[nt]);
+          }
+        }
+        stage(BUF ^ 1, u);
         __builtin_amdgcn_sched_barrier(0);
       });
       __builtin_amdgcn_s_setprio(0);
@@ -800,7 +857,11 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      ke[p] = exp_of(k_exp[p]);
+      if (kOnePage) {
+        kcur = knext;
+        knext = 127 + k_exp[p];
+      }
+      ke[p] = k_exp[p];
       ve[p] = exp_of(v_exp[p]);
       tiles[p] = tile_of(entry[p]);
     }
@@ -842,7 +903,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
     uint32_t next[NP];
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      ke[p] = exp_of(kexp[tiles[p]]);
+      ke[p] = kexp[tiles[p]];
+      if (kOnePage) kcur = 127 + ke[p];
       ve[p] = exp_of(vexp[tiles[p]]);
       tiles[p] = tile_of(entry_at(row_of(k0 + kKeys, p)));
       next[p] = tile_of(entry_at(row_of(k0 + 2 * kKeys, p)));
@@ -852,7 +914,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
     fetch(k0 + kKeys);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      ke[p] = exp_of(kexp[tiles[p]]);
+      ke[p] = kexp[tiles[p]];
+      if (kOnePage) knext = 127 + ke[p];
       ve[p] = exp_of(vexp[tiles[p]]);
       tiles[p] = next[p];
     }

@@ -353,6 +353,24 @@ def test_attn_large_tiles_are_the_same_on_every_run():
         assert torch.equal(first, call_attn(c, 100, 0))
 
 
+def test_attn_large_tiles_of_uneven_rows():
+    """Q rows of very different size, with a few large channels, zeros, and a NaN row that stays alone."""
+    c = attn_case([3000], [150], 64, 8, 8, seed=2)
+    g = torch.Generator().manual_seed(3)
+    q = c["q"].float().cpu() * torch.exp(1.5 * torch.randn((1, 8, 150, 1), generator=g).clamp(-2, 1))
+    q[..., 5] *= 12
+    q[0, 3, 7] = 0
+    q[0, 2, 9, 1:] *= 2.0**-20
+    c["q"] = q.to(torch.bfloat16).to(DEV)
+    check_attn(c, 1, 0)
+    want = call_attn(c, 1, 0)
+    c["q"][0, 1, 2, 77] = float("nan")
+    got = call_attn(c, 1, 0)
+    assert got[0, 1, 2].isnan().all()
+    got[0, 1, 2] = want[0, 1, 2]
+    assert torch.equal(got, want)
+
+
 def test_attn_wrong_estimate_of_the_longest_stream():
     """max_q chooses the kernel and nothing else."""
     c = attn_case([3000, 40], [120, 2], 64, 8, 8)

@@ -352,9 +352,9 @@ hipError_t launch_cache_store(StoreArgs a) {
   const dim3 grid((unsigned)((units + 3) / 4));
   // Rows held: small windows go with calls of many single tokens, whose waves should all be
   // resident (16 rows: eight waves a SIMD); where windows hold whole runs, reading a run
-  // once counts (the page: two waves, one with 128). 3042 rows of 40 heads in pages of
+  // once counts (the page: two waves, one with 128). 3041 rows of 40 heads in pages of
   // 64 / 128: 20.2 / 29.9 us held whole, 29.2 in 16 rows / 34.5 in 64; 256 single tokens of
-  // 40 heads: 11.2 with 16 rows held, 14.9 with 32, 26.6 with 64; 3042 rows of 5 heads
+  // 40 heads: 11.2 with 16 rows held, 14.9 with 32, 26.6 with 64; 3041 rows of 5 heads
   // (short windows, whole runs): 12.3, 10.3, 9.9.
   if (a.window < 16)
     launch_store<16>(a, grid);

@@ -436,9 +436,10 @@ typedef struct fva_rope_params {
  * place); any other overlap is the caller's error. dtype: the type of all
  * four. ids: device int32, or NULL. No workspace.
  * Errors: FVA_ERR_INVALID_ARG (NULL or misaligned pointers, dtype, pairing,
- * theta), FVA_ERR_SHAPE (extents, odd or too many channels, rows that overlap
- * or do not start on 16-byte boundaries), FVA_ERR_UNSUPPORTED (head_dim !=
- * 128, batch or heads > 65535, R % 16 under FVA_ROPE_HALVES).
+ * inverse, theta), FVA_ERR_SHAPE (extents, odd or too many channels, rows
+ * that overlap or do not start on 16-byte boundaries), FVA_ERR_UNSUPPORTED
+ * (head_dim != 128, batch or heads of Q and K together > 65535, 2^31 tokens,
+ * R % 16 under FVA_ROPE_HALVES).
  */
 fva_status fva_rope(const void* Q, void* Q_out, const fva_qkv_desc* q_desc, const void* K, void* K_out,
                     const fva_qkv_desc* k_desc, int32_t dtype, const fva_rope_params* params, const int32_t* ids,
@@ -453,7 +454,8 @@ fva_status fva_rope(const void* Q, void* Q_out, const fva_qkv_desc* q_desc, cons
  * head: the value of a code is E4M3(code) * 2^e, with e = max(-100, min{e :
  * amax * 2^-e <= 448}) over the page's tokens of that head. Token j of stream
  * s lies in page block_table[s, j / page] at j % page; block_table is int32
- * [streams, table_width]. All of it is the caller's memory.
+ * [streams, table_width]. All of it is the caller's memory. A pool has fewer
+ * than 2^31 slots and 2^29 page heads (pages * heads).
  *
  * One step: fva_cache_plan gives the new tokens their pages, fva_rope turns Q
  * and K by the plan's ids, fva_cache_store writes K and V to the plan's slots,
@@ -520,7 +522,7 @@ fva_status fva_cache_plan(const int32_t* held, const int32_t* fresh, int32_t str
  * cache holds no NaN, and a masked key cannot reach any output.
  * Errors: FVA_ERR_INVALID_ARG (NULL or misaligned pointers), FVA_ERR_SHAPE
  * (heads differ, bad extents or strides), FVA_ERR_UNSUPPORTED (head_dim,
- * page, 2^31 slots or more, batch * tokens * heads >= 2^30).
+ * page, a larger pool, batch * tokens * heads >= 2^30).
  */
 fva_status fva_cache_store(const void* K, const void* V, const fva_qkv_desc* desc, const int32_t* slots,
                            const fva_cache* cache, void* stream);
@@ -558,7 +560,8 @@ fva_status fva_attn_cache_workspace_size(const fva_qkv_desc* q_desc, const fva_c
  * Errors: FVA_ERR_INVALID_ARG (NULL or misaligned pointers, negative max_q,
  * frame or window, scale), FVA_ERR_SHAPE (batch != 1, heads not a multiple of
  * the cache's, overlapping rows), FVA_ERR_UNSUPPORTED (head_dim, page,
- * table_width * page >= 2^30, 2^31 rows or work items), FVA_ERR_WORKSPACE.
+ * a larger pool, table_width * page >= 2^30, 2^31 rows or work items),
+ * FVA_ERR_WORKSPACE.
  */
 fva_status fva_attn_cache(const void* Q, const fva_qkv_desc* q_desc, const fva_cache* cache,
                           const int32_t* block_table, int32_t table_width, const int32_t* kv_len,

@@ -9,15 +9,16 @@
 // Rows are taken per K/V head: the heads / kv_heads query heads that share a K/V head lie
 // next to each other, row = token * group + head in the group, in tiles of kRows rows.
 // Work item = (tile, chunk of its keys), one workgroup per item and K/V head. The chunk
-// length follows from the lengths on the device (make_split), the same in every wave of
-// both kernels: as many items as the chip holds workgroups, where the tiles alone are
-// fewer. A tile in several chunks leaves unnormalised partial results that
+// length follows from the lengths on the device (work_of), the same in every wave of the
+// attention and the merge: as many items as the chip holds workgroups, where the tiles
+// alone are fewer. A tile in several chunks leaves unnormalised partial results that
 // cache_combine_kernel merges in chunk order (no atomics: the result is the same on
 // every run).
 //
 // Codes enter the products exactly (E4M3 has four significant bits; bf16 holds them times
-// the page's power of two); accumulation, statistics and sums are fp32. P is rounded to bf16 for its product with V, as the matrix unit takes it: at
-// most half a step, 2^-9, of each term, the same as the output's own rounding.
+// the page's power of two); accumulation, statistics and sums are fp32. P is rounded to
+// bf16 for its product with V, as the matrix unit takes it: at most half a step, 2^-8 of
+// each term, the same as the output's own rounding.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -44,12 +45,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kRows = 16;        // query rows of a small tile: one MFMA column each
 constexpr int kBigRows = 128;    // query rows of a large tile: 32 for each wave
 constexpr int kKeys = 64;        // keys a wave takes at a time
-constexpr int kWaves = 4;        // waves of a workgroup, each on every fourth 64 keys
-constexpr int kCacheSlots = 2048; // workgroups to split for, small tiles
-constexpr int kBigSlots = 512;    // large tiles: two a CU, as many as are resident
+constexpr int kWaves = 4;        // waves of a workgroup (small tiles of few keys: 1 to 8)
+constexpr int kCacheSlots = 2048;  // workgroups to split for, small tiles
+constexpr int kBigSlots = 512;     // large tiles: two a CU, as many as are resident
 constexpr int kXcds = 8;
-constexpr int kMostChunks = 128;  // of a tile
-constexpr int kMinChunk = kWaves * kKeys;  // a shorter chunk leaves waves without keys
+constexpr int kMostChunks = 128;   // of a tile
+constexpr int kMinChunk = kWaves * kKeys;  // a shorter chunk leaves a small tile's waves without keys
 
 typedef __attribute__((address_space(4))) const int32_t const_i32;
 
@@ -523,9 +524,9 @@ __device__ __forceinline__ float exp2_arg(float s, float c2, float negm) {
 // bits, which two codes of four hold, q = (high + low / 16) * 2^e with e from the row's
 // largest element. high is q rounded, low what that left, times 16: exact down to 2^-13 of
 // the row's maximum, and off by at most 2^-21 of it below (half of low's smallest step,
-// 2^-14, against a maximum above 224). Two fp8 products take the time of one in bf16 and spare K's
-// conversion and half of its LDS traffic: 4680 rows against 32,760 keys (40 heads) 2713 ->
-// 2499 us.
+// 2^-14, against a maximum above 224). Two fp8 products take the time of one in bf16 and
+// spare K's conversion and half of its LDS traffic: 4680 rows against 32,760 keys (40
+// heads) 2713 -> 2499 us.
 //
 // O^T += V^T P^T in bf16: P would need two codes too, and their making is vector work, of
 // which there is no less than of matrix work (36 + 16 products a wave and step of 16 passes
@@ -734,8 +735,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   asm volatile("" : "+v"(kaddr[0]), "+v"(kaddr[1]), "+v"(wk), "+v"(wv[0]), "+v"(wv[1]));
 
   // One step: S^T, under it the next step's codes into the other buffer and the loads of the
-  // step after that, the softmax, O^T += V^T P^T. (The two buffers are two copies of the code: their offsets are
-  // immediate.)
+  // step after that, the softmax, O^T += V^T P^T. (The two buffers are two copies of the
+  // code: their offsets are immediate.)
   auto step = [&](auto buf_c, int base) {
     constexpr int BUF = decltype(buf_c)::value;
     auto kfrag = [&](int t) {

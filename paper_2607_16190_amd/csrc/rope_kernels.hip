@@ -13,7 +13,7 @@
 // two decimals), its sine and cosine are taken in 32 bits.
 //
 // Bound by memory: every element is read and written once (40 + 40 heads of 720p, 3.1 GB:
-// 568 us, 5.45 TB/s; a plain copy of 1 GiB reaches 5.08). All heads of a token share its
+// 568 us, 5.45 TB/s; a plain copy of 1 GiB reaches 5.13). All heads of a token share its
 // angles, so a thread owns eight pairs of one token, forms their sines and cosines once
 // and goes through a group of heads with them in registers.
 #include <hip/hip_runtime.h>

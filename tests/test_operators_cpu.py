@@ -122,6 +122,17 @@ def test_attn_refusals():
     assert attn(streams=0) == fva.FVA_OK
 
 
+@pytest.mark.parametrize("pages, heads", [((1 << 27) + 1, 2), (1 << 28, 2), (1 << 14, 1 << 15), (1, 1 << 29)])
+def test_pools_of_too_many_page_heads(pages, heads):
+    """Pages times heads, and slots, past what the kernels index with 32 bits: refused by every call that takes a pool."""
+    for page in (16, 128):
+        c = cache(pages=pages, heads=heads, page=page)
+        assert store(d=desc(H=heads), c=c) == fva.FVA_ERR_UNSUPPORTED
+        assert attn(d=desc(H=heads), c=c) == fva.FVA_ERR_UNSUPPORTED
+        with pytest.raises(fva.FvaError):
+            fva.fva_attn_cache_workspace_size(desc(H=heads), c, 1, 1, 1)
+
+
 def test_attn_workspace_size():
     n = fva.fva_attn_cache_workspace_size(desc(N=1), cache(), 100, 1, 1)
     assert n > 0 and n % 4 == 0

@@ -9,11 +9,11 @@
 // Rows are taken per K/V head: the heads / kv_heads query heads that share a K/V head lie
 // next to each other, row = token * group + head in the group, in tiles of kRows rows.
 // Work item = (tile, chunk of its keys), one workgroup per item and K/V head. The chunk
-// length follows from the lengths on the device (work_of), the same in every wave of the
-// attention and the merge: as many items as the chip holds workgroups, where the tiles
-// alone are fewer. A tile in several chunks leaves unnormalised partial results that
-// cache_combine_kernel merges in chunk order (no atomics: the result is the same on
-// every run).
+// length follows from the lengths on the device (work_of), the same in every wave: as many
+// items as the chip holds workgroups, where the tiles alone are fewer (of large tiles, as
+// many as fill whole rounds of workgroups). A tile in several chunks leaves unnormalised
+// partial results that cache_combine_kernel merges in chunk order (no atomics: the result
+// is the same on every run).
 //
 // Codes enter the products exactly (E4M3 has four significant bits; bf16 holds them times
 // the page's power of two); accumulation, statistics and sums are fp32. P is rounded to
@@ -47,7 +47,9 @@ constexpr int kBigRows = 128;    // query rows of a large tile: 32 for each wave
 constexpr int kKeys = 64;        // keys a wave takes at a time
 constexpr int kWaves = 4;        // waves of a workgroup (small tiles of few keys: 1 to 8)
 constexpr int kCacheSlots = 2048;  // workgroups to split for, small tiles
-constexpr int kBigSlots = 512;     // large tiles: two a CU, as many as are resident
+constexpr int kBigSlots = 512;     // large tiles: two a CU, as many as are resident (a round)
+constexpr int kBigRounds = 5;      // that their chunks may take
+constexpr int kDeal = 64;          // chunks that are dealt from one end of a head's to the other (32: 82 us for 69.6 below)
 constexpr int kXcds = 8;
 constexpr int kMostChunks = 128;   // of a tile
 constexpr int kMinChunk = kWaves * kKeys;  // a shorter chunk leaves a small tile's waves without keys
@@ -93,6 +95,18 @@ __device__ __forceinline__ int chunks_of(int span, int chunk) {
   return (int)min(max(1u, ((uint32_t)span + (uint32_t)chunk - 1u) / (uint32_t)chunk), (uint32_t)kMostChunks);
 }
 
+// The largest value of the wave, in every lane.
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t b) {
+  b = max(b, dpp_move<0xB1>(b));
+  b = max(b, dpp_move<0x4E>(b));
+  b = max(b, dpp_move<0x141>(b));
+  b = max(b, dpp_move<0x140>(b));
+  const auto p = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  b = max(p[0], p[1]);
+  const auto q = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return max(q[0], q[1]);
+}
+
 // What a wave knows of the whole call: the streams over its lanes, the first 64 of them
 // in registers (the others are looked at again).
 struct Work {
@@ -111,36 +125,92 @@ __device__ __forceinline__ Stream stream_in(const CacheAttnArgs& P, int s, int c
   return r;
 }
 
-// Longest chunk: the tiles' keys over the P.slots workgroups there are to fill. Large tiles
-// run in rounds of as many workgroups as are resident, so theirs grows until the chunks fit
-// the rounds (a few left over would take a round of their own). A stream's keys are then
-// cut into equal chunks of at most that (chunk_keys). Every sum is of integers: each wave of
-// both kernels comes to the same numbers.
+// Chunk length of large tiles. They run in rounds of as many workgroups as are resident, the
+// last of which may be nearly empty: 13 tiles of 40 heads, 520 workgroups of 537 steps, took
+// 1400 us as they are, 1140 / 1057 / 1023 in two / three / four chunks each. Each lane
+// estimates one length: those that fill one round, two, ... and longer ones, and the tiles as
+// they are. The end of the rounds is the mean workgroup's steps and its way in for each, what
+// the longest has more, and the merge. Of more than 64 streams, whose lengths even out, the
+// mean is taken. (Integers but for reciprocals and their products, which round alike
+// everywhere: every wave comes to the same length.)
+__device__ __forceinline__ int big_chunk(const CacheAttnArgs& P, const Work& w, uint64_t total, int lane) {
+  constexpr int kNever = INT32_MAX / 2;
+  constexpr int kWayIn = 12;           // steps that a workgroup's start costs
+  constexpr int kLengths = 12;         // tried for a number of rounds, by a tenth longer each
+  auto tiles_by = [&](auto f) {  // the sum of tiles * f(stream)
+    uint64_t n = (uint64_t)w.mine.tiles * (uint64_t)f(w.mine);
+    for (int s = lane + kWave; s < P.streams; s += kWave) {
+      const Stream r = stream_of(P, s);
+      n += (uint64_t)r.tiles * (uint64_t)f(r);
+    }
+    return wave_sum_u64(n);
+  };
+  const uint64_t tiles = tiles_by([](const Stream&) { return 1; });
+  if (tiles == 0 || tiles > (uint64_t)P.slots) return kNever;  // (P.slots, some thousand: the products below fit)
+  const uint64_t steps64 = total / kKeys;
+  const int even = (int)min(steps64 * (uint32_t)P.kv_heads / kBigSlots + 1, (uint64_t)1 << 24);  // steps of each of a round's places
+  int n = even;
+  if (P.streams <= kWave) {
+    const int r = 1 + lane / kLengths, k = lane % kLengths;
+    n = max((even + r - 1) / r, kMinChunk / kKeys);
+    n = lane >= kBigRounds * kLengths ? 1 << 24 : n + n * k / 10;
+    const float inv = __builtin_amdgcn_rcpf((float)n);
+    const int mine = (w.mine.mean + kKeys - 1) / kKeys;
+    const int longest = min((int)wave_max_u32((uint32_t)mine), n);
+    int items = 0;
+    for (int s0 = 0; s0 < P.streams; s0 += 4) {  // (lanes past the streams have no tiles)
+#pragma unroll
+      for (int s = s0; s < s0 + 4; ++s) {
+        const int c = (int)((float)(__builtin_amdgcn_readlane(mine, s) + n - 1) * inv);
+        items += __builtin_amdgcn_readlane(w.mine.tiles, s) * min(max(c, 1), kMostChunks);
+      }
+    }
+    const int mean = (int)((float)min(steps64, (uint64_t)1 << 30) * __builtin_amdgcn_rcpf((float)items));
+    const int rounds = (items * P.kv_heads + kBigSlots - 1) / kBigSlots;
+    int cost = rounds * (mean + kWayIn) + max(longest - mean, 0);
+    if (items > (int)tiles) cost += 5 + items * P.kv_heads / 64;
+    if (items > P.slots) cost = INT32_MAX;
+    uint32_t key = ~((uint32_t)min(cost, (1 << 26) - 1) << 6 | (uint32_t)lane);
+    key = wave_max_u32(key);
+    const int best = 63 - (int)(key & 63);
+    n = __builtin_amdgcn_readlane(n, best);
+  } else {
+    n = max(even, kMinChunk / kKeys);
+  }
+  if (n >= 1 << 24) return kNever;
+  const int chunk = n * kKeys;
+  return tiles_by([&](const Stream& st) { return chunks_of(st.span, chunk); }) <= (uint64_t)P.slots ? chunk : kNever;
+}
+
+// Longest chunk: of small tiles, the tiles' keys over the P.slots workgroups there are to
+// fill. A stream's keys are then cut into equal chunks of at most that (chunk_keys). Every
+// sum is of integers: each wave of the attention and the merge comes to the same numbers.
+// The merge has the length from the attention (kFound), which leaves it behind the partial
+// results.
+enum class Tiles { kSmall, kBig, kFound };
+template <Tiles TILES>
 __device__ __forceinline__ Work work_of(const CacheAttnArgs& P, int lane) {
   constexpr int kNever = INT32_MAX / 2;
   Work w;
   w.mine = lane < P.streams ? stream_of(P, lane) : none();
   w.chunk = kNever;
   if (P.slots) {
-    uint64_t total = (uint64_t)w.mine.tiles * (uint64_t)w.mine.mean;
-    for (int s = lane + kWave; s < P.streams; s += kWave) {
-      const Stream r = stream_of(P, s);
-      total += (uint64_t)r.tiles * (uint64_t)r.mean;
-    }
-    total = wave_sum_u64(total);
-    const double units = ceil((double)total * P.inv_slots * (1.0 / kKeys));
-    if (units < kNever / kKeys / 8) {
-      int n = max((int)units, kMinChunk / kKeys);
-      for (int tries = 0; P.rows == kBigRows && tries < 10; ++tries) {
-        uint64_t items = (uint64_t)w.mine.tiles * (uint64_t)chunks_of(w.mine.mean, n * kKeys);
-        for (int s = lane + kWave; s < P.streams; s += kWave) {
-          const Stream r = stream_of(P, s);
-          items += (uint64_t)r.tiles * (uint64_t)chunks_of(r.mean, n * kKeys);
-        }
-        if (wave_sum_u64(items) <= (uint64_t)P.slots) break;
-        n += max(n >> 3, 1);
+    if constexpr (TILES == Tiles::kFound) {
+      w.chunk = *P.chunk;
+    } else {
+      uint64_t total = (uint64_t)w.mine.tiles * (uint64_t)w.mine.mean;
+      for (int s = lane + kWave; s < P.streams; s += kWave) {
+        const Stream r = stream_of(P, s);
+        total += (uint64_t)r.tiles * (uint64_t)r.mean;
       }
-      w.chunk = n * kKeys;
+      total = wave_sum_u64(total);
+      if constexpr (TILES == Tiles::kBig) {
+        w.chunk = big_chunk(P, w, total, lane);
+      } else {
+        const double units = ceil((double)total * P.inv_slots * (1.0 / kKeys));
+        if (units < kNever / kKeys / 8) w.chunk = max((int)units * kKeys, kMinChunk);
+      }
+      if (blockIdx.x == 0 && threadIdx.x == 0) *P.chunk = w.chunk;
     }
     w.mine.chunks = chunks_of(w.mine.span, w.chunk);
   }
@@ -297,7 +367,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
   const int g = lane >> 4, l = lane & 15;
   const int item = divide(blockIdx.x, P.by_heads);
   const int kh = (int)blockIdx.x - item * P.kv_heads;
-  const Work work = work_of(P, lane);
+  const Work work = work_of<Tiles::kSmall>(P, lane);
   const Item it = item_of(P, work, item, lane);
   if (it.stream < 0) return;
   const Stream& st = it.st;
@@ -544,17 +614,24 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, l = lane & 15;
 
-  // Work items head by head, the runs of consecutive ones on one XCD (workgroups go to the
-  // XCDs in turn): the tiles of a head read its keys out of one L2. Later tiles first: with
-  // causal frames they see the most keys.
-  const Work work = work_of(P, lane);
+  // Work items head by head, in runs of which each is one XCD's (workgroups go to the XCDs in
+  // turn): the tiles of a head read its keys out of one L2. Later tiles first: with causal
+  // frames they see the most keys. Chunks, of which two of a CU run side by side and a head's
+  // may be several XCDs', are dealt besides, every total / 64th of them and then the next, so
+  // that neighbours, which are alike, do not all meet in one place: six streams of 558 to
+  // 5760 keys (2727 rows, 12 / 4 heads) 93.2 -> 69.6 us, with windows 83.7 -> 67.7, one
+  // stream of 14,040 keys causal by frame (5 heads) 134 either way.
+  const Work work = work_of<Tiles::kBig>(P, lane);
   const int total = (int)min((int64_t)work.items, P.items_per_head);
   const int64_t all = (int64_t)total * P.kv_heads;
   const int64_t run = (all + kXcds - 1) / kXcds;
   const int64_t index = (blockIdx.x % kXcds) * run + blockIdx.x / kXcds;
   if (total <= 0 || blockIdx.x / kXcds >= run || index >= all) return;
   const int kh = (int)((uint32_t)index / (uint32_t)total);
-  const int item = total - 1 - (int)(index - (int64_t)kh * total);
+  const int nth = (int)(index - (int64_t)kh * total);
+  const int deal = nth & (kDeal - 1);
+  const int dealt = deal * (total / kDeal) + min(deal, total & (kDeal - 1)) + nth / kDeal;
+  const int item = total - 1 - (P.slots ? dealt : nth);
   const Item it = item_of(P, work, item, lane);
   if (it.stream < 0) return;
   const Stream& st = it.st;
@@ -1040,7 +1117,7 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   const int part = blockIdx.x & ((1 << part_shift) - 1);
   const int tile_id = divide(blockIdx.x >> part_shift, P.by_heads);
   const int kh = (int)(blockIdx.x >> part_shift) - tile_id * P.kv_heads;
-  const Work work = work_of(P, lane);
+  const Work work = work_of<Tiles::kFound>(P, lane);
   // the stream that holds tile tile_id, its first tile and its first item
   int tiles = 0, item0 = 0, stream = -1;
   Stream st;
@@ -1119,7 +1196,7 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   }
 }
 
-// Workgroups per K/V head to split for (0: the tiles alone fill the device), and the items
+// Workgroups per K/V head to split for (large tiles: at most; 0: not split), and the items
 // there can be.
 struct Sizes {
   bool big;
@@ -1144,14 +1221,17 @@ Sizes sizes_of(bool big, int tokens, int heads, int kv_heads, int streams, int64
   r.keys = most_keys;
   if (window) r.keys = std::min(most_keys, (int64_t)window + 2 * (int64_t)frame + r.rows + kKeys);
   // Chunks do not pay for a second launch that merges them where keys are few (large tiles:
-  // ten steps), nor from two rounds of tiles on.
-  const int round = std::max(1, (big ? kBigSlots : kCacheSlots) / kv_heads);
+  // ten steps), nor where the tiles, not split, fill two rounds.
   const int64_t full = ((int64_t)tokens * group + r.rows - 1) / r.rows;  // tiles if the rows fill them
-  const bool few = big ? r.keys <= 10 * kKeys : few_keys(r.keys);
-  r.slots = few || full >= 2 * (int64_t)round ? 0 : (full > round ? 2 : 1) * round;
-  // The sum of chunks_of(mean) is at most slots + tiles, and chunks_of(span) at most twice
-  // that, equal where the mean is the span (always for small tiles).
-  r.items = r.slots ? (big ? 2 : 1) * (r.tiles + r.slots) : r.tiles;
+  if (big) {
+    const int64_t places = std::max(1, (full * kv_heads > kBigSlots ? kBigRounds : 2) * kBigSlots / kv_heads);
+    r.slots = r.keys <= 10 * kKeys || 2 * full > places ? 0 : (int)places;
+    r.items = std::max(r.tiles, std::min((int64_t)r.slots, r.tiles * std::min<int64_t>(kMostChunks, (r.keys + kMinChunk - 1) / kMinChunk)));
+  } else {
+    const int round = std::max(1, kCacheSlots / kv_heads);
+    r.slots = few_keys(r.keys) || full >= 2 * (int64_t)round ? 0 : (full > round ? 2 : 1) * round;
+    r.items = r.tiles + r.slots;  // the sum of chunks_of(span)
+  }
   return r;
 }
 
@@ -1183,11 +1263,13 @@ int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int m
   return most;
 }
 
+static size_t partial_floats(const Sizes& z, int kv_heads) { return (size_t)z.items * kv_heads * z.rows * (kHeadDim + 2); }
+
 size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
   size_t most = 0;
   for (int big = 0; big <= ((int64_t)max_q * (heads / kv_heads) > kRows ? 1 : 0); ++big) {
     const Sizes z = sizes_of(big, tokens, heads, kv_heads, streams, most_keys, 0, 0);
-    if (z.slots) most = std::max(most, (size_t)z.items * kv_heads * z.rows * (kHeadDim + 2) * sizeof(float));
+    if (z.slots) most = std::max(most, (partial_floats(z, kv_heads) + 1) * sizeof(float));
   }
   return most;
 }
@@ -1226,6 +1308,7 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
   a.slots = z.slots;
   a.inv_slots = z.slots ? 1.0 / z.slots : 0.0;
   a.items = z.items * a.kv_heads;
+  a.chunk = z.slots ? reinterpret_cast<int32_t*>(a.partial + partial_floats(z, a.kv_heads)) : nullptr;
   // Small tiles of few keys: as many waves a tile as the chip has room for (twelve a CU) when
   // all tiles run at once. Of many keys: four, and codes that no other workgroup of
   // the call reads go past the caches (64 ragged streams of up to 16000 keys, 8 heads: 165 ->

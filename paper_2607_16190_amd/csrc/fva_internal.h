@@ -174,7 +174,8 @@ struct CacheAttnArgs {
   // set by the launcher
   int group = 1;       // query heads per K/V head
   int rows = 16, row_shift = 4;  // query rows of a tile, a power of two
-  int slots = 0;       // workgroups per K/V head that the keys are split for; 0: not split
+  int slots = 0;       // workgroups per K/V head that the keys are split for (large tiles: at most); 0: not split
+  int32_t* chunk = nullptr;  // the chunk length the attention came to, for the merge
   double inv_slots = 0.0;  // 1 / slots
   bool ramp = false;   // rows of a stream see more and more keys: its tiles are weighed by their mean
   int64_t items = 0;   // items, and partial results, there is room for

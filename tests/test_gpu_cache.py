@@ -341,6 +341,25 @@ def test_attn_large_tiles_of_many_streams(streams):
     check_attn(attn_case(lens, [int(n) for n in rng.integers(0, 40, streams)], 16, 8, 2, seed=streams), 1, 0)
 
 
+@pytest.mark.parametrize("frame", [0, 1])
+@pytest.mark.parametrize("lens,rows,page", [([8000], [1100], 128), ([6000, 77, 4500], [700, 50, 400], 32)])
+def test_attn_large_tiles_of_more_than_a_round(lens, rows, page, frame):
+    """More tiles than run at once, whose keys are split all the same: the first and the last rows of every stream."""
+    c = attn_case(lens, rows, page, 64, 1, seed=sum(lens) + frame)
+    got = bits(call_attn(c, frame))[0].transpose(1, 0, 2)
+    assert np.isfinite(got).all()
+    q = bits(c["q"])[0].transpose(1, 0, 2)
+    at = 0
+    for s, (n, m) in enumerate(zip(lens, rows)):
+        k, v = (cached(*c[x], c["table"][s], n) for x in "kv")
+        some = min(m, 25)
+        # the first rows are the newest of a stream that ends with them
+        for first, end in ((at, n - (m - some) if frame else n), (at + m - some, n)):
+            O, mass, reach = attn_ref(q[first: first + some], k[:end], v[:end], frame)
+            assert (np.abs(got[first: first + some] - O) <= attn_tolerance(O, mass, reach)).all(), (s, first)
+        at += m
+
+
 def test_attn_large_tiles_without_a_merge():
     """As many tiles as the device holds twice over."""
     check_attn(attn_case([1500], [1500], 64, 100, 50, seed=1), 500, 700)

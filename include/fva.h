@@ -528,8 +528,9 @@ fva_status fva_cache_store(const void* K, const void* V, const fva_qkv_desc* des
                            const fva_cache* cache, void* stream);
 
 /* Workspace bytes of fva_attn_cache: the partial results of tiles whose keys
- * are split over workgroups, none (0) where the rows alone fill the device.
- * Host only. */
+ * are split over workgroups (up to 170 MB, in batches of few rows a stream 8 KB
+ * for each stream and K/V head besides), none (0) where the rows alone fill
+ * the device. Host only. */
 fva_status fva_attn_cache_workspace_size(const fva_qkv_desc* q_desc, const fva_cache* cache, int32_t table_width,
                                          int32_t streams, int32_t max_q, size_t* bytes);
 

@@ -1144,7 +1144,7 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   if (n_chunks == 1) return;
   const int64_t first = ((int64_t)item0 + (int64_t)tile * st.chunks) * P.kv_heads + kh;
   // (sums past 32 bits, from starts that are not ascending)
-  if (tile < 0 || tile >= st.tiles || item0 < 0 || first + (int64_t)(n_chunks - 1) * P.kv_heads >= P.items) return;
+  if (tile < 0 || tile >= st.tiles || item0 < 0 || first + (int64_t)(n_chunks - 1) * P.kv_heads >= P.partials) return;
   const int64_t size = P.rows * (kHeadDim + 2);
   const float* base = P.partial + first * size;
   const int64_t step = P.kv_heads * size;
@@ -1202,6 +1202,7 @@ struct Sizes {
   bool big;
   int rows, slots;
   int64_t tiles, items;
+  int64_t partials;  // items that there are at most where they are split
   int64_t keys;  // that any tile sees, at most
 };
 // Streams of few keys stay in one workgroup a tile: up to four turns of eight waves.
@@ -1225,12 +1226,15 @@ Sizes sizes_of(bool big, int tokens, int heads, int kv_heads, int streams, int64
   const int64_t full = ((int64_t)tokens * group + r.rows - 1) / r.rows;  // tiles if the rows fill them
   if (big) {
     const int64_t places = std::max(1, (full * kv_heads > kBigSlots ? kBigRounds : 2) * kBigSlots / kv_heads);
-    r.slots = r.keys <= 10 * kKeys || 2 * full > places ? 0 : (int)places;
-    r.items = std::max(r.tiles, std::min((int64_t)r.slots, r.tiles * std::min<int64_t>(kMostChunks, (r.keys + kMinChunk - 1) / kMinChunk)));
+    const int64_t most = r.tiles * std::min<int64_t>(kMostChunks, (r.keys + kMinChunk - 1) / kMinChunk);
+    r.slots = r.keys <= 10 * kKeys || 2 * full > places ? 0 : (int)std::min(places, most);
+    r.items = std::max(r.tiles, (int64_t)r.slots);
+    r.partials = r.slots;  // big_chunk splits into no more
   } else {
     const int round = std::max(1, kCacheSlots / kv_heads);
     r.slots = few_keys(r.keys) || full >= 2 * (int64_t)round ? 0 : (full > round ? 2 : 1) * round;
     r.items = r.tiles + r.slots;  // the sum of chunks_of(span)
+    r.partials = r.items;
   }
   return r;
 }
@@ -1263,7 +1267,7 @@ int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int m
   return most;
 }
 
-static size_t partial_floats(const Sizes& z, int kv_heads) { return (size_t)z.items * kv_heads * z.rows * (kHeadDim + 2); }
+static size_t partial_floats(const Sizes& z, int kv_heads) { return (size_t)z.partials * kv_heads * z.rows * (kHeadDim + 2); }
 
 size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
   size_t most = 0;
@@ -1305,6 +1309,7 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
   a.by_heads = divisor_of(a.kv_heads);
   a.by_frame = divisor_of(std::max(a.frame, 1));
   a.items_per_head = z.items;
+  a.partials = z.partials * a.kv_heads;
   a.slots = z.slots;
   a.inv_slots = z.slots ? 1.0 / z.slots : 0.0;
   a.items = z.items * a.kv_heads;

@@ -452,7 +452,8 @@ fva_status fva_rope(const void* Q, void* Q_out, const fva_qkv_desc* q_desc, cons
  * codes k8, v8 uint8 [pages, heads, page, 128] (OCP E4M3) and exponents
  * k_exp, v_exp int32 [pages, heads], one power-of-two scale for each page and
  * head: the value of a code is E4M3(code) * 2^e, with e = max(-100, min{e :
- * amax * 2^-e <= 448}) over the page's tokens of that head. Token j of stream
+ * amax * 2^-e <= 448}) over the page's tokens of that head, which is at most
+ * 120 (the e of infinities). Token j of stream
  * s lies in page block_table[s, j / page] at j % page; block_table is int32
  * [streams, table_width]. All of it is the caller's memory. A pool has fewer
  * than 2^31 slots and 2^29 page heads (pages * heads).
@@ -518,8 +519,9 @@ fva_status fva_cache_plan(const int32_t* held, const int32_t* fresh, int32_t str
  * on the page's new scale. The rows of one page must be one run in a call, as
  * fva_cache_plan lays them out; a page that appears in two runs of one call
  * (the same slot twice among them) ends with unspecified contents.
- * Infinities are stored as the largest code, NaN as some finite value: the
- * cache holds no NaN, and a masked key cannot reach any output.
+ * Infinities are stored as the largest code (+-448 * 2^120), NaN as some
+ * finite value: the cache holds no NaN, and a masked key, whatever its values,
+ * cannot reach any output.
  * Errors: FVA_ERR_INVALID_ARG (NULL or misaligned pointers), FVA_ERR_SHAPE
  * (heads differ, bad extents or strides), FVA_ERR_UNSUPPORTED (head_dim,
  * page, a larger pool, batch * tokens * heads >= 2^30).

@@ -16,7 +16,7 @@
 // is the same on every run).
 //
 // Codes enter the products exactly (E4M3 has four significant bits; bf16 holds them times
-// the page's power of two); accumulation, statistics and sums are fp32. P is rounded to
+// the page's power of two; V's times 2^-kValueDown of it, see there); accumulation, statistics and sums are fp32. P is rounded to
 // bf16 for its product with V, as the matrix unit takes it: at most half a step, 2^-8 of
 // each term, the same as the output's own rounding.
 #include <hip/hip_runtime.h>
@@ -53,6 +53,14 @@ constexpr int kDeal = 64;          // chunks that are dealt from one end of a he
 constexpr int kXcds = 8;
 constexpr int kMostChunks = 128;   // of a tile
 constexpr int kMinChunk = kWaves * kKeys;  // a shorter chunk leaves a small tile's waves without keys
+// V enters its product on 2^-kValueDown of its scale, and O is scaled back where it is written.
+// A page's scale reaches 2^120 (a value above 448 * 2^119, an infinity), on which codes from 256
+// on are no finite bf16 numbers: an infinity there would meet the P = 0 of a row that does not
+// see its key, and 0 * inf is NaN. Sixteen binades down, the largest value is 1.75 * 2^112, and
+// the smallest code of the smallest scale, 2^(-9 - 100 - 16), is still a normal number.
+constexpr int kValueDown = 16;
+constexpr float kValueUp = 65536.f;
+static_assert(kValueUp == (float)(1 << kValueDown) && kCacheExpMin - 9 - kValueDown >= -126);
 
 typedef __attribute__((address_space(4))) const int32_t const_i32;
 
@@ -328,6 +336,12 @@ __device__ __forceinline__ bf16x8 eight_bf16(uint32_t lo, uint32_t hi, float sca
 // 2^e of a stored exponent, which lies in [kCacheExpMin, 120].
 __device__ __forceinline__ float exp_of(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
+// The scale of V in its product.
+__device__ __forceinline__ float value_exp(int e) { return exp_of(e - kValueDown); }
+
+// What turns a row's sum of P V into O.
+__device__ __forceinline__ float out_scale(float sum) { return sum > 0.f ? 1.0f / sum * kValueUp : 0.f; }
+
 // max over lanes l, l^16, l^32, l^48, and the sum of them.
 __device__ __forceinline__ float max4(float v) {
   const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -421,7 +435,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
     for (int t = 0; t < 4; ++t) {
       const uint32_t at = (uint32_t)min(max(entry[t], 0), P.pages - 1) * (uint32_t)P.kv_heads + (uint32_t)kh;
       ke[t] = exp_of(((const const_i32*)P.k_exp)[at]);
-      ve[t] = exp_of(((const const_i32*)P.v_exp)[at]);
+      ve[t] = value_exp(((const const_i32*)P.v_exp)[at]);
       const uint8_t* kp = P.k8 + (uint64_t)at * (uint32_t)(P.page * kHeadDim);
       const uint8_t* vp = P.v8 + (uint64_t)at * (uint32_t)(P.page * kHeadDim);
       const int kr = min(max(base + 16 * t + l, it.lo), k1 - 1) & (P.page - 1);
@@ -540,7 +554,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
       for (int e = 0; e < 8; ++e) acc[e] += f * ot[w][orow][oc + e];
     }
     if (n_chunks == 1) {
-      const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+      const float inv = out_scale(sum);
       const int out_tok = divide(out_row, P.by_group);
       const int oh = kh * P.group + out_row - out_tok * P.group;
       uint16_t* dst = static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + out_tok) * P.stride_n + (int64_t)oh * P.stride_h + oc;
@@ -940,7 +954,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
         knext = 127 + k_exp[p];
       }
       ke[p] = k_exp[p];
-      ve[p] = exp_of(v_exp[p]);
+      ve[p] = value_exp(v_exp[p]);
       tiles[p] = tile_of(entry[p]);
     }
     if (act) {
@@ -983,7 +997,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
     for (int p = 0; p < NP; ++p) {
       ke[p] = kexp[tiles[p]];
       if (kOnePage) kcur = 127 + ke[p];
-      ve[p] = exp_of(vexp[tiles[p]]);
+      ve[p] = value_exp(vexp[tiles[p]]);
       tiles[p] = tile_of(entry_at(row_of(k0 + kKeys, p)));
       next[p] = tile_of(entry_at(row_of(k0 + 2 * kKeys, p)));
     }
@@ -994,7 +1008,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
     for (int p = 0; p < NP; ++p) {
       ke[p] = kexp[tiles[p]];
       if (kOnePage) knext = 127 + ke[p];
-      ve[p] = exp_of(vexp[tiles[p]]);
+      ve[p] = value_exp(vexp[tiles[p]]);
       tiles[p] = next[p];
     }
     __syncthreads();
@@ -1012,7 +1026,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
     const int row = row0 + 16 * nt + l;
     if (row >= rows) continue;
     if (n_chunks == 1) {
-      const float inv = lsum[nt][0] > 0.f ? 1.0f / lsum[nt][0] : 0.f;
+      const float inv = out_scale(lsum[nt][0]);
       const int tok = divide(row, P.by_group);
       const int qh = kh * P.group + row - tok * P.group;
       uint16_t* out = static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + tok) * P.stride_n + (int64_t)qh * P.stride_h + 4 * g;
@@ -1152,7 +1166,7 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   auto put = [&](int r, float sum, float2 o) {
     const int row = tile * P.rows + r;
     if (row >= rows) return;
-    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+    const float inv = out_scale(sum);
     const int tok = divide(row, P.by_group);
     const int qh = kh * P.group + row - tok * P.group;
     bf16x2 v;

@@ -1,0 +1,79 @@
+"""A cached V value as large as the format holds, infinities among them, reaches no row that does not see its key."""
+
+import numpy as np
+import pytest
+
+import paper_2607_16190_amd as fva
+from oracle.stream import attn_ref, attn_tolerance, cached, visible_keys
+from test_gpu_cache import DEV, bits, i32
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+BF16_MAX = float(torch.finfo(torch.bfloat16).max)
+
+# keys, rows, heads, K/V heads, frame, window, token, whether large tiles of 128 rows take it. The token is the newest
+# one, or lies where the window of some rows has left it. Small tiles: split where the table holds more than 2048 keys.
+# Large ones: more than 4096 turns of 16 rows x 64 keys, 16384 up to 2048 keys; split from 640 keys on.
+CASES = {
+    "small": (49, 8, 2, 2, 1, 0, 48, False),
+    "small, window": (300, 12, 4, 2, 1, 40, 251, False),
+    "small, split": (3009, 5, 2, 2, 1, 0, 3008, False),
+    "large": (577, 577, 64, 64, 1, 0, 576, True),
+    "large, split": (4545, 150, 8, 2, 1, 0, 4544, True),
+    "large, split, window, frames": (4545, 150, 16, 4, 7, 2500, 1950, True),
+}
+
+
+def stored(n, page, KH, token, value, seed):
+    """A cache of n tokens in pages out of order whose V is `value` in some channels of one token."""
+    g = torch.Generator().manual_seed(seed)
+    k, v = (torch.randn((1, KH, n, 128), generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    v[:, :, token, 3:77:5] = value
+    need = -(-n // page)
+    table = np.random.default_rng(seed).permutation(need + 2)[:need]
+    slots = table[np.arange(n) // page] * page + np.arange(n) % page
+    k8, v8 = (torch.zeros((need + 2, KH, page, 128), dtype=torch.uint8, device=DEV) for _ in range(2))
+    ke, ve = (torch.zeros((need + 2, KH), dtype=torch.int32, device=DEV) for _ in range(2))
+    fva.fva_cache_store(k, v, i32(slots), k8, v8, ke, ve)
+    return k8, v8, ke, ve, table, (int(table[token // page]), token % page)
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), 3.38e38])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("name", CASES)
+def test_huge_value_of_a_masked_key(name, page, value):
+    n, m, H, KH, frame, window, token, large = CASES[name]
+    k8, v8, ke, ve, table, (at, off) = stored(n, page, KH, token, value, n + page)
+    q = torch.randn((1, m, H, 128), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(DEV).transpose(1, 2)
+
+    def attend(v8, max_q=m):
+        return fva.fva_attn_cache(q, k8, v8, ke, ve, i32(table[None]), i32([n]), i32([0, m]), max_q, frame=frame, window=window)
+
+    got = attend(v8)
+    plain = v8.clone()
+    plain[at, :, off] = 0  # the same cache and scales but for that token
+    want = attend(plain)
+    bounds = [visible_keys(n, m, i, frame, window) for i in range(m)]
+    sees = np.array([lo <= token < hi for lo, hi in bounds])
+    assert sees.any() and not sees.all()
+    blind = torch.from_numpy(~sees)
+    assert want.isfinite().all()
+    assert torch.equal(got[:, :, blind], want[:, :, blind])
+    # another kernel sums in another order
+    assert torch.equal(want, attend(plain, 0)) != large
+    # the rows that see it, some of them: past bf16's range an infinity of the right sign
+    rows = np.flatnonzero(sees)[:8]
+    first, end = rows[0], rows[-1] + 1
+    host = [(c.cpu().numpy(), e.cpu().numpy()) for c, e in ((k8, ke), (v8, ve))]
+    kk, vv = (cached(c, e, table, n) for c, e in host)
+    x = bits(q)[0].transpose(1, 0, 2)
+    for i in range(first, end):
+        lo, hi = bounds[i]
+        O, mass, reach = attn_ref(x[i: i + 1], kk[lo:hi], vv[lo:hi])
+        tol = attn_tolerance(O, mass, reach)
+        y = bits(got)[0].transpose(1, 0, 2)[i: i + 1]
+        with np.errstate(invalid="ignore"):
+            near = np.abs(y - O) <= tol
+        past = np.isinf(y) & (np.sign(y) == np.sign(O)) & (np.abs(O) + tol > BF16_MAX)
+        assert (near | past).all(), i

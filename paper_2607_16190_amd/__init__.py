@@ -529,9 +529,16 @@ def _stream_on(dev: int, stream):
     return _stream_ptr(stream) if raw is None else raw(dev)
 
 
-def _int32(t, what, n):
-    if t.dtype is not _I32 or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous int32 tensor of {n} entries")
+def _int32(t, what, *shape):
+    if t.dtype is not _I32 or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor of shape {shape}")
+
+
+def _table_width(table, streams) -> int:
+    """Columns of a block table, which has a row for each stream."""
+    width = table.shape[-1] if table.dim() else 0
+    _int32(table, "block_table", streams, width)
+    return width
 
 
 def _rows_of(x) -> _Desc:
@@ -595,7 +602,7 @@ def fva_rope(q, k, hw, dims, *, ids=None, origin=(0, 0, 0), theta: float = 10000
             _int32(ids, "ids", qd.tokens)
         else:
             ids_stride = qd.tokens
-            _int32(ids, "ids", qd.batch * ids_stride)
+            _int32(ids, "ids", qd.batch, ids_stride)
     rows, cols = hw
     dim_t, dim_y, dim_x = dims
     t0, y0, x0 = origin
@@ -617,12 +624,11 @@ def fva_cache_plan(held, fresh, state, ring, block_table, page: int, tokens: int
     """
     dev = _same_device(held, fresh, state, ring, block_table)
     n, cap = held.numel(), ring.numel()
-    width = block_table.shape[-1]
     _int32(held, "held", n)
     _int32(fresh, "fresh", n)
     _int32(state, "state", 3)
     _int32(ring, "ring", cap)
-    _int32(block_table, "block_table", n * width)
+    width = _table_width(block_table, n)
     sizes = (n, n + 1, tokens, tokens, 3)
     if out is None:
         if tokens < 0:
@@ -651,16 +657,16 @@ def _cache_of(k8, v8, k_exp, v_exp) -> _Cache:
     if not k8.is_contiguous() or not v8.is_contiguous():
         raise ValueError("k8 and v8 must be contiguous")
     pages, heads, page, d = shape
-    _int32(k_exp, "k_exp", pages * heads)
-    _int32(v_exp, "v_exp", pages * heads)
+    _int32(k_exp, "k_exp", pages, heads)
+    _int32(v_exp, "v_exp", pages, heads)
     return _Cache(pages, heads, page, d, k8.data_ptr(), v8.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr())
 
 
 def fva_cache_store(k, v, slots, k8, v8, k_exp, v_exp, *, stream=None):
     """K and V rows into the cache's slots, in place (see include/fva.h).
 
-    k, v: bf16 [batch, heads, tokens, 128]; slots: int32, one per (batch, token); k8, v8: uint8 [pages, heads, page,
-    128]; k_exp, v_exp: int32 [pages, heads].
+    k, v: bf16 [batch, heads, tokens, 128]; slots: int32 [batch * tokens] or [batch, tokens]; k8, v8: uint8 [pages,
+    heads, page, 128]; k_exp, v_exp: int32 [pages, heads].
     """
     if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
         raise ValueError("k and v must be bf16")
@@ -668,7 +674,10 @@ def fva_cache_store(k, v, slots, k8, v8, k_exp, v_exp, *, stream=None):
         raise ValueError("k and v must share shape and strides")
     dev = _same_device(k, v, slots, k8, v8, k_exp, v_exp)
     desc = _rows_of(k)
-    _int32(slots, "slots", desc.batch * desc.tokens)
+    if slots.dim() == 1:
+        _int32(slots, "slots", desc.batch * desc.tokens)
+    else:
+        _int32(slots, "slots", desc.batch, desc.tokens)
     cache = _cache_of(k8, v8, k_exp, v_exp)
     st = lib.fva_cache_store(k.data_ptr(), v.data_ptr(), ctypes.byref(desc), slots.data_ptr(), ctypes.byref(cache),
                              _stream_on(dev, stream))
@@ -709,8 +718,7 @@ def fva_attn_cache(q, k8, v8, k_exp, v_exp, block_table, kv_len, q_start, max_q:
     n = kv_len.numel()
     _int32(kv_len, "kv_len", n)
     _int32(q_start, "q_start", n + 1)
-    width = block_table.shape[-1]
-    _int32(block_table, "block_table", n * width)
+    width = _table_width(block_table, n)
     if out is None:
         out = _like(q, stream)
     else:

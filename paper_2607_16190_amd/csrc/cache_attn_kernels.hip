@@ -135,16 +135,23 @@ __device__ __forceinline__ Stream stream_in(const CacheAttnArgs& P, int s, int c
 
 // Chunk length of large tiles. They run in rounds of as many workgroups as are resident, the
 // last of which may be nearly empty: 13 tiles of 40 heads, 520 workgroups of 537 steps, took
-// 1400 us as they are, 1140 / 1057 / 1023 in two / three / four chunks each. Each lane
+// 1400 us as they are, 1140 / 1057 / 1023 in two / three / four chunks each (without frames;
+// causal by frame 1478 us as they are, 1090 as chosen here). Each lane
 // estimates one length: those that fill one round, two, ... and longer ones, and the tiles as
 // they are. The end of the rounds is the mean workgroup's steps and its way in for each, what
-// the longest has more, and the merge. Of more than 64 streams, whose lengths even out, the
-// mean is taken. (Integers but for reciprocals and their products, which round alike
-// everywhere: every wave comes to the same length.)
+// the longest has more, and the merge. The workgroups of a length are estimated from the
+// tiles' mean keys, whether there is room for its partial results is counted from the widest
+// ones': causal chunks have fewer on average, and a length without room is no choice. (One
+// stream, causal by frame, 5 heads, 4680 rows, 32,760 keys: 606 us as 185 workgroups, 363
+// split; 8 heads, 1560 rows, 61,560 keys 1114 -> 389.) Of more than 64 streams, whose lengths even out, the mean is
+// taken. (Integers but for reciprocals and their products, which round alike everywhere:
+// every wave comes to the same length.)
 __device__ __forceinline__ int big_chunk(const CacheAttnArgs& P, const Work& w, uint64_t total, int lane) {
   constexpr int kNever = INT32_MAX / 2;
   constexpr int kWayIn = 12;           // steps that a workgroup's start costs
   constexpr int kLengths = 12;         // tried for a number of rounds, by a tenth longer each
+  constexpr int kWhole = 1 << 24;      // steps, no less than any tile has: the tiles as they are
+  constexpr int kNoRoom = (1 << 26) - 1;  // more than any cost
   auto tiles_by = [&](auto f) {  // the sum of tiles * f(stream)
     uint64_t n = (uint64_t)w.mine.tiles * (uint64_t)f(w.mine);
     for (int s = lane + kWave; s < P.streams; s += kWave) {
@@ -156,37 +163,40 @@ __device__ __forceinline__ int big_chunk(const CacheAttnArgs& P, const Work& w, 
   const uint64_t tiles = tiles_by([](const Stream&) { return 1; });
   if (tiles == 0 || tiles > (uint64_t)P.slots) return kNever;  // (P.slots, some thousand: the products below fit)
   const uint64_t steps64 = total / kKeys;
-  const int even = (int)min(steps64 * (uint32_t)P.kv_heads / kBigSlots + 1, (uint64_t)1 << 24);  // steps of each of a round's places
-  int n = even;
+  const int even = (int)min(steps64 * (uint32_t)P.kv_heads / kBigSlots + 1, (uint64_t)kWhole);  // steps of each of a round's places
   if (P.streams <= kWave) {
     const int r = 1 + lane / kLengths, k = lane % kLengths;
-    n = max((even + r - 1) / r, kMinChunk / kKeys);
-    n = lane >= kBigRounds * kLengths ? 1 << 24 : n + n * k / 10;
-    const float inv = __builtin_amdgcn_rcpf((float)n);
+    int n = max((even + r - 1) / r, kMinChunk / kKeys);
+    n = lane >= kBigRounds * kLengths ? kWhole : n + n * k / 10;
+    const float inv = __builtin_amdgcn_rcpf((float)n) * (1.f + 0x1p-20f);
     const int mine = (w.mine.mean + kKeys - 1) / kKeys;
+    const int most = (w.mine.span + kKeys - 1) / kKeys;
     const int longest = min((int)wave_max_u32((uint32_t)mine), n);
-    int items = 0;
+    // The chunks that all tiles are cut into: of the streams' means, and of their spans. (No
+    // quotient comes out too small: inv is above 1 / n by more than all roundings.)
+    int items = 0, room = 0;
     for (int s0 = 0; s0 < P.streams; s0 += 4) {  // (lanes past the streams have no tiles)
 #pragma unroll
       for (int s = s0; s < s0 + 4; ++s) {
-        const int c = (int)((float)(__builtin_amdgcn_readlane(mine, s) + n - 1) * inv);
-        items += __builtin_amdgcn_readlane(w.mine.tiles, s) * min(max(c, 1), kMostChunks);
+        const int tiles_s = __builtin_amdgcn_readlane(w.mine.tiles, s);
+        auto cut = [&](int steps) { return tiles_s * min(max((int)((float)(steps + n - 1) * inv), 1), kMostChunks); };
+        room += cut(__builtin_amdgcn_readlane(most, s));
+        if (P.ramp) items += cut(__builtin_amdgcn_readlane(mine, s));
       }
     }
+    if (!P.ramp) items = room;
     const int mean = (int)((float)min(steps64, (uint64_t)1 << 30) * __builtin_amdgcn_rcpf((float)items));
     const int rounds = (items * P.kv_heads + kBigSlots - 1) / kBigSlots;
     int cost = rounds * (mean + kWayIn) + max(longest - mean, 0);
     if (items > (int)tiles) cost += 5 + items * P.kv_heads / 64;
-    if (items > P.slots) cost = INT32_MAX;
-    uint32_t key = ~((uint32_t)min(cost, (1 << 26) - 1) << 6 | (uint32_t)lane);
+    cost = room > P.slots && n < kWhole ? kNoRoom : min(cost, kNoRoom - 1);
+    uint32_t key = ~((uint32_t)cost << 6 | (uint32_t)lane);
     key = wave_max_u32(key);
     const int best = 63 - (int)(key & 63);
     n = __builtin_amdgcn_readlane(n, best);
-  } else {
-    n = max(even, kMinChunk / kKeys);
+    return n >= kWhole ? kNever : n * kKeys;
   }
-  if (n >= 1 << 24) return kNever;
-  const int chunk = n * kKeys;
+  const int chunk = max(even, kMinChunk / kKeys) * kKeys;
   return tiles_by([&](const Stream& st) { return chunks_of(st.span, chunk); }) <= (uint64_t)P.slots ? chunk : kNever;
 }
 

@@ -143,9 +143,13 @@ __device__ __forceinline__ Stream stream_in(const CacheAttnArgs& P, int s, int c
 // tiles' mean keys, whether there is room for its partial results is counted from the widest
 // ones': causal chunks have fewer on average, and a length without room is no choice. (One
 // stream, causal by frame, 5 heads, 4680 rows, 32,760 keys: 606 us as 185 workgroups, 363
-// split; 8 heads, 1560 rows, 61,560 keys 1114 -> 389.) Of more than 64 streams, whose lengths even out, the mean is
-// taken. (Integers but for reciprocals and their products, which round alike everywhere:
-// every wave comes to the same length.)
+// split; 8 heads, 1560 rows, 61,560 keys 1114 -> 389.) Of more than 64 streams, whose lengths
+// even out, the length that fills one round is taken, or, without room for it, the one that
+// room is certain for: a tile of more than one chunk has fewer than 2 * span / length. Tiles
+// that stay whole need no room, so that a long stream among many short ones is split however
+// many there are (100 streams of 32 rows and up to 300 keys, one of 100,000, 8 heads: 1704 us
+// whole, 96 split). (Integers but for reciprocals and their products, which round alike
+// everywhere: every wave comes to the same length.)
 __device__ __forceinline__ int big_chunk(const CacheAttnArgs& P, const Work& w, uint64_t total, int lane) {
   constexpr int kNever = INT32_MAX / 2;
   constexpr int kWayIn = 12;           // steps that a workgroup's start costs
@@ -160,11 +164,11 @@ __device__ __forceinline__ int big_chunk(const CacheAttnArgs& P, const Work& w, 
     }
     return wave_sum_u64(n);
   };
-  const uint64_t tiles = tiles_by([](const Stream&) { return 1; });
-  if (tiles == 0 || tiles > (uint64_t)P.slots) return kNever;  // (P.slots, some thousand: the products below fit)
   const uint64_t steps64 = total / kKeys;
   const int even = (int)min(steps64 * (uint32_t)P.kv_heads / kBigSlots + 1, (uint64_t)kWhole);  // steps of each of a round's places
   if (P.streams <= kWave) {
+    const int tiles = (int)wave_sum_u64((uint64_t)w.mine.tiles);
+    if (tiles == 0) return kNever;
     const int r = 1 + lane / kLengths, k = lane % kLengths;
     int n = max((even + r - 1) / r, kMinChunk / kKeys);
     n = lane >= kBigRounds * kLengths ? kWhole : n + n * k / 10;
@@ -172,23 +176,24 @@ __device__ __forceinline__ int big_chunk(const CacheAttnArgs& P, const Work& w, 
     const int mine = (w.mine.mean + kKeys - 1) / kKeys;
     const int most = (w.mine.span + kKeys - 1) / kKeys;
     const int longest = min((int)wave_max_u32((uint32_t)mine), n);
-    // The chunks that all tiles are cut into: of the streams' means, and of their spans. (No
-    // quotient comes out too small: inv is above 1 / n by more than all roundings.)
+    // The chunks that all tiles are cut into, of the streams' means, and those with a partial
+    // result, of their spans. (No quotient comes out too small: inv is above 1 / n by more than
+    // all roundings.)
     int items = 0, room = 0;
     for (int s0 = 0; s0 < P.streams; s0 += 4) {  // (lanes past the streams have no tiles)
 #pragma unroll
       for (int s = s0; s < s0 + 4; ++s) {
         const int tiles_s = __builtin_amdgcn_readlane(w.mine.tiles, s);
         auto cut = [&](int steps) { return tiles_s * min(max((int)((float)(steps + n - 1) * inv), 1), kMostChunks); };
-        room += cut(__builtin_amdgcn_readlane(most, s));
-        if (P.ramp) items += cut(__builtin_amdgcn_readlane(mine, s));
+        const int widest = cut(__builtin_amdgcn_readlane(most, s));
+        room += widest > tiles_s ? widest : 0;
+        items += P.ramp ? cut(__builtin_amdgcn_readlane(mine, s)) : widest;
       }
     }
-    if (!P.ramp) items = room;
     const int mean = (int)((float)min(steps64, (uint64_t)1 << 30) * __builtin_amdgcn_rcpf((float)items));
     const int rounds = (items * P.kv_heads + kBigSlots - 1) / kBigSlots;
     int cost = rounds * (mean + kWayIn) + max(longest - mean, 0);
-    if (items > (int)tiles) cost += 5 + items * P.kv_heads / 64;
+    if (items > tiles) cost += 5 + items * P.kv_heads / 64;
     cost = room > P.slots && n < kWhole ? kNoRoom : min(cost, kNoRoom - 1);
     uint32_t key = ~((uint32_t)cost << 6 | (uint32_t)lane);
     key = wave_max_u32(key);
@@ -196,9 +201,19 @@ __device__ __forceinline__ int big_chunk(const CacheAttnArgs& P, const Work& w, 
     n = __builtin_amdgcn_readlane(n, best);
     return n >= kWhole ? kNever : n * kKeys;
   }
-  const int chunk = max(even, kMinChunk / kKeys) * kKeys;
-  return tiles_by([&](const Stream& st) { return chunks_of(st.span, chunk); }) <= (uint64_t)P.slots ? chunk : kNever;
+  const int one = max(even, kMinChunk / kKeys);
+  if (one >= kWhole) return kNever;
+  const uint64_t room = tiles_by([&](const Stream& st) {
+    const int c = chunks_of(st.span, one * kKeys);
+    return c > 1 ? c : 0;
+  });
+  if (room <= (uint64_t)P.slots) return one * kKeys;
+  const double sure = (double)tiles_by([](const Stream& st) { return st.span; }) * P.inv_slots * (2.0 / kKeys) + 1.0;
+  return sure < kWhole ? (int)sure * kKeys : kNever;
 }
+
+// Places of a stream's partial results: tiles in one chunk leave none.
+__device__ __forceinline__ int parts_of(const Stream& st) { return st.chunks > 1 ? st.tiles * st.chunks : 0; }
 
 // Longest chunk: of small tiles, the tiles' keys over the P.slots workgroups there are to
 // fill. A stream's keys are then cut into equal chunks of at most that (chunk_keys). Every
@@ -283,11 +298,12 @@ struct Item {
   Stream st;
   int tile, n_chunks, k0, k1;
   int lo;      // first key that any row sees
+  int part;    // its partial result's place, where the tile is in several chunks
 };
 __device__ __forceinline__ Item item_of(const CacheAttnArgs& P, const Work& w, int item, int lane) {
   Item r;
   r.stream = -1;
-  int before = 0;  // items of the streams before the one that is found
+  int before = 0, parts = 0;  // items, and partial results, of the streams before the one that is found
   for (int s0 = 0; s0 < P.streams; s0 += kWave) {
     const Stream mine = s0 ? stream_in(P, s0 + lane, w.chunk) : w.mine;
     const int upto = s0 ? wave_incl_scan_i32(mine.tiles * mine.chunks, lane) : w.upto;
@@ -297,19 +313,23 @@ __device__ __forceinline__ Item item_of(const CacheAttnArgs& P, const Work& w, i
       r.stream = s0 + l;
       r.st = lane_stream(mine, l);
       before += __builtin_amdgcn_readlane(upto, l) - r.st.tiles * r.st.chunks;
+      if (r.st.chunks > 1) parts += __builtin_amdgcn_readlane(wave_incl_scan_i32(parts_of(mine), lane), l) - parts_of(r.st);
       break;
     }
     before += __builtin_amdgcn_readlane(upto, 63);
+    if (P.slots) parts += __builtin_amdgcn_readlane(wave_incl_scan_i32(parts_of(mine), lane), 63);
   }
   if (r.stream < 0) return r;
   const int at = item - before;
   int chunk = 0;
   r.tile = at;
+  r.part = parts + at;
   if (r.st.chunks > 1) {
     r.tile = (int)((uint32_t)at / (uint32_t)r.st.chunks);
     chunk = at - r.tile * r.st.chunks;
   }
-  if (at < 0 || r.tile >= r.st.tiles) {  // (sums past 32 bits, from starts that are not ascending)
+  // (sums past 32 bits, from starts that are not ascending)
+  if (at < 0 || r.tile >= r.st.tiles || (r.st.chunks > 1 && (uint32_t)r.part >= (uint32_t)P.partials)) {
     r.stream = -1;
     return r;
   }
@@ -570,7 +590,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void cache_attn_kernel(CacheAttnA
       uint16_t* dst = static_cast<uint16_t*>(P.O) + (int64_t)(st.q0 + out_tok) * P.stride_n + (int64_t)oh * P.stride_h + oc;
       *reinterpret_cast<bf16x8*>(dst) = __builtin_convertvector(acc * inv, bf16x8);
     } else {
-      float* part = P.partial + ((int64_t)item * P.kv_heads + kh) * (kRows * (kHeadDim + 2));
+      float* part = P.partial + ((int64_t)it.part * P.kv_heads + kh) * (kRows * (kHeadDim + 2));
       *reinterpret_cast<f32x8*>(part + orow * kHeadDim + oc) = acc;
       if (oc == 0) {
         part[kRows * kHeadDim + orow] = m;
@@ -1044,7 +1064,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void cache_attn_big_kernel(Cache
       for (int mt = 0; mt < 8; ++mt)
         *reinterpret_cast<bf16x4*>(out + 16 * mt) = __builtin_convertvector(o[mt][nt] * inv, bf16x4);
     } else {
-      float* part = P.partial + ((int64_t)item * P.kv_heads + kh) * (kBigRows * (kHeadDim + 2));
+      float* part = P.partial + ((int64_t)it.part * P.kv_heads + kh) * (kBigRows * (kHeadDim + 2));
       const int r = row - tile * kBigRows;
 #pragma unroll
       for (int mt = 0; mt < 8; ++mt) *reinterpret_cast<f32x4*>(part + r * kHeadDim + 16 * mt + 4 * g) = o[mt][nt];
@@ -1142,12 +1162,12 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
   const int tile_id = divide(blockIdx.x >> part_shift, P.by_heads);
   const int kh = (int)(blockIdx.x >> part_shift) - tile_id * P.kv_heads;
   const Work work = work_of<Tiles::kFound>(P, lane);
-  // the stream that holds tile tile_id, its first tile and its first item
-  int tiles = 0, item0 = 0, stream = -1;
+  // the stream that holds tile tile_id, its first tile and its first partial result
+  int tiles = 0, part0 = 0, stream = -1;
   Stream st;
   for (int s0 = 0; s0 < P.streams; s0 += kWave) {
     const Stream mine = s0 ? stream_in(P, s0 + lane, work.chunk) : work.mine;
-    const int upto = s0 ? wave_incl_scan_i32(mine.tiles * mine.chunks, lane) : work.upto;
+    const int upto = wave_incl_scan_i32(parts_of(mine), lane);
     const int tiles_upto = wave_incl_scan_i32(mine.tiles, lane);
     const uint64_t past = __ballot(tiles + tiles_upto > tile_id);
     if (past) {
@@ -1155,22 +1175,22 @@ __global__ __launch_bounds__(256) void cache_combine_kernel(CacheAttnArgs P) {
       stream = s0 + l;
       st = lane_stream(mine, l);
       tiles += __builtin_amdgcn_readlane(tiles_upto, l) - st.tiles;
-      item0 += __builtin_amdgcn_readlane(upto, l) - st.tiles * st.chunks;
+      part0 += __builtin_amdgcn_readlane(upto, l) - parts_of(st);
       break;
     }
     tiles += __builtin_amdgcn_readlane(tiles_upto, 63);
-    item0 += __builtin_amdgcn_readlane(upto, 63);
+    part0 += __builtin_amdgcn_readlane(upto, 63);
   }
   if (stream < 0 || st.chunks == 1) return;
   const int tile = tile_id - tiles;
   const Span span = tile_span(P, st, tile);
   const int n_chunks = chunks_of(span.end - span.begin, chunk_keys(P, st));
   if (n_chunks == 1) return;
-  const int64_t first = ((int64_t)item0 + (int64_t)tile * st.chunks) * P.kv_heads + kh;
+  const int64_t first = (int64_t)part0 + (int64_t)tile * st.chunks;
   // (sums past 32 bits, from starts that are not ascending)
-  if (tile < 0 || tile >= st.tiles || item0 < 0 || first + (int64_t)(n_chunks - 1) * P.kv_heads >= P.partials) return;
+  if (tile < 0 || tile >= st.tiles || part0 < 0 || first + n_chunks > P.partials) return;
   const int64_t size = P.rows * (kHeadDim + 2);
-  const float* base = P.partial + first * size;
+  const float* base = P.partial + (first * P.kv_heads + kh) * size;
   const int64_t step = P.kv_heads * size;
   const int rows = st.q_len * P.group;
   auto put = [&](int r, float sum, float2 o) {
@@ -1226,7 +1246,7 @@ struct Sizes {
   bool big;
   int rows, slots;
   int64_t tiles, items;
-  int64_t partials;  // items that there are at most where they are split
+  int64_t partials;  // partial results that there are at most (below 2^31, as the items)
   int64_t keys;  // that any tile sees, at most
 };
 // Streams of few keys stay in one workgroup a tile: up to four turns of eight waves.
@@ -1252,8 +1272,9 @@ Sizes sizes_of(bool big, int tokens, int heads, int kv_heads, int streams, int64
     const int64_t places = std::max(1, (full * kv_heads > kBigSlots ? kBigRounds : 2) * kBigSlots / kv_heads);
     const int64_t most = r.tiles * std::min<int64_t>(kMostChunks, (r.keys + kMinChunk - 1) / kMinChunk);
     r.slots = r.keys <= 10 * kKeys || 2 * full > places ? 0 : (int)std::min(places, most);
-    r.items = std::max(r.tiles, (int64_t)r.slots);
-    r.partials = r.slots;  // big_chunk splits into no more
+    // big_chunk splits into no more than r.slots; tiles of one stream are split all or not at all
+    r.items = streams > 1 ? r.tiles + r.slots : std::max(r.tiles, (int64_t)r.slots);
+    r.partials = r.slots;
   } else {
     const int round = std::max(1, kCacheSlots / kv_heads);
     r.slots = few_keys(r.keys) || full >= 2 * (int64_t)round ? 0 : (full > round ? 2 : 1) * round;
@@ -1333,7 +1354,7 @@ hipError_t launch_cache_attn(CacheAttnArgs a) {
   a.by_heads = divisor_of(a.kv_heads);
   a.by_frame = divisor_of(std::max(a.frame, 1));
   a.items_per_head = z.items;
-  a.partials = z.partials * a.kv_heads;
+  a.partials = (int)z.partials;
   a.slots = z.slots;
   a.inv_slots = z.slots ? 1.0 / z.slots : 0.0;
   a.items = z.items * a.kv_heads;

@@ -179,7 +179,7 @@ struct CacheAttnArgs {
   double inv_slots = 0.0;  // 1 / slots
   bool ramp = false;   // rows of a stream see more and more keys: its tiles are weighed by their mean
   int64_t items = 0;   // items there can be
-  int64_t partials = 0;  // partial results there is room for
+  int partials = 0;    // partial results there is room for, per K/V head
   int64_t items_per_head = 0;
   int most_keys = 0;   // that any tile sees, at most
   Divisor by_group, by_heads, by_frame;

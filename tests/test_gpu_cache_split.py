@@ -67,3 +67,28 @@ def test_causal_chunks_are_split(H, rows, keys, frame):
 @pytest.mark.parametrize("keys", range(6000, 33000, 2700))
 def test_a_share_of_heads_is_split_at_every_length(keys):
     assert run([keys], [4680], 5, 5, 1560)
+
+
+@pytest.mark.parametrize("frame", [0, 1])
+@pytest.mark.parametrize("streams,H,keys,at", [(100, 8, 100000, 0), (100, 8, 100000, 57), (30, 40, 30000, 11), (64, 8, 60000, 63), (65, 8, 60000, 64)])
+def test_a_long_stream_among_many_short_ones_is_split(streams, H, keys, at, frame):
+    """More tiles than there are places for partial results, or streams than a wave has lanes: the short ones leave none."""
+    lens = [300 + (7 * s) % 50 for s in range(streams)]
+    lens[at] = keys
+    assert run(lens, [32 - s % 3 for s in range(streams)], H, H, frame, seed=at)
+
+
+@pytest.mark.parametrize("frame", [0, 1, 450])
+def test_many_streams_that_one_round_has_no_room_for(frame):
+    """The mean of causal rows is half of their widest: twice as many chunks as estimated."""
+    run([900] * 66, [900] * 66, 1, 1, frame, page=16)
+    lens, rows = [900] * 66, [900] * 66
+    lens[40] = 20000
+    assert run(lens, rows, 1, 1, frame, page=16)
+
+
+def test_long_and_short_streams_in_turn():
+    """Partial results of split streams with unsplit ones between them, on both sides of the 64th."""
+    lens = [9000 if s % 9 == 4 else 200 + 3 * s for s in range(100)]
+    assert run(lens, [33] * 100, 16, 4, 1)
+    assert run(lens[:60], [33] * 60, 16, 4, 1)

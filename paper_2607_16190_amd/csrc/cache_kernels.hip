@@ -148,24 +148,25 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs P) {
     P.state_out[1] = count - taken + pushed;
     P.state_out[2] = refused_s;
   }
-  const int step = gridDim.x * kPlanThreads;
-  const int i0 = blockIdx.x * kPlanThreads + threadIdx.x;
-  for (int i = i0; i < taken; i += step) {
-    const int s = find_stream(first, S, i);
-    const int col = pages_of(held_s[s]) + i - first[s];
+  // (Unsigned: the step past the last of up to 2^31 - 1 rows or pages is no negative index.)
+  const uint32_t step = gridDim.x * kPlanThreads;
+  const uint32_t i0 = blockIdx.x * kPlanThreads + threadIdx.x;
+  for (uint32_t i = i0; i < (uint32_t)taken; i += step) {
+    const int s = find_stream(first, S, (int)i);
+    const int col = pages_of(held_s[s]) + (int)i - first[s];
     P.table[(int64_t)s * P.width + col] = P.ring[((int64_t)head + i) % cap];
   }
-  for (int i = i0; i < pushed; i += step) {
-    const int s = find_stream(behind, S, i);
-    P.ring[((int64_t)head + count + i) % cap] = P.table[(int64_t)s * P.width + i - behind[s]];
+  for (uint32_t i = i0; i < (uint32_t)pushed; i += step) {
+    const int s = find_stream(behind, S, (int)i);
+    P.ring[((int64_t)head + count + i) % cap] = P.table[(int64_t)s * P.width + (int)i - behind[s]];
   }
-  for (int r = i0; r < P.tokens; r += step) {
+  for (uint32_t r = i0; r < (uint32_t)P.tokens; r += step) {
     int slot = -1, id = -1;
-    if (r < rows) {
-      const int s = find_stream(q_start, S, r);
+    if (r < (uint32_t)rows) {
+      const int s = find_stream(q_start, S, (int)r);
       const int held = held_s[s];
       if (held >= 0) {
-        id = held + r - q_start[s];
+        id = held + (int)r - q_start[s];
         const int col = id / P.page, now = pages_of(held);
         const int page = col < now ? P.table[(int64_t)s * P.width + col] : P.ring[((int64_t)head + first[s] + col - now) % cap];
         slot = page < 0 ? -1 : page * P.page + id % P.page;
@@ -335,7 +336,7 @@ hipError_t launch_cache_plan(const PlanArgs& a) {
   (void)hipGetLastError();
   // Four rows a thread; the ring entries of a call are fewer than its token rows or are
   // gone through by the same loop.
-  const int grid = std::min(256, std::max(1, (a.tokens + 4 * kPlanThreads - 1) / (4 * kPlanThreads)));
+  const int grid = (int)std::min<int64_t>(256, std::max<int64_t>(1, ((int64_t)a.tokens + 4 * kPlanThreads - 1) / (4 * kPlanThreads)));
   cache_plan_kernel<<<grid, kPlanThreads, 0, a.stream>>>(a);
   return hipGetLastError();
 }

@@ -43,6 +43,9 @@ struct Elem<f32x8> { typedef float type; };
 constexpr int kRopeThreads = 256;
 constexpr int kRopeTokens = 32;  // eight threads per token, each 16 channels in two vectors
 constexpr int kRopeUnroll = 4;   // heads in flight per thread
+// Tokens of a launch: 2^32 threads and more in a row of workgroups are cut to 32 bits without an
+// error (2^29 + 5 tokens ran as 32).
+constexpr int64_t kRopeMost = (int64_t)1 << 28;
 
 struct RopeParams {
   RopeTensor q, k;
@@ -56,6 +59,7 @@ struct RopeParams {
   const int32_t* ids;
   int64_t ids_stride;
   int heads_per_group;  // heads (of Q and K together) a workgroup goes through
+  int n0;               // first token of the launch
 };
 
 // The products that are fused with the sum are named, so that every copy of the code the
@@ -126,10 +130,11 @@ __device__ __forceinline__ void turn_heads(const RopeTensor& x, int b, int n, in
 
 template <typename V, bool STREAM>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams P) {
-  const int n = blockIdx.x * kRopeTokens + (int)(threadIdx.x >> 3);
+  const uint32_t nth = (uint32_t)P.n0 + blockIdx.x * kRopeTokens + (threadIdx.x >> 3);
   const int unit = threadIdx.x & 7;
   const int b = blockIdx.z;
-  if (n >= P.tokens) return;
+  if (nth >= (uint32_t)P.tokens) return;
+  const int n = (int)nth;
   const int id = P.ids ? P.ids[(int64_t)b * P.ids_stride + n] : n;
 
   // The thread's two vectors of eight channels and their eight pairs. Halves: unit u
@@ -202,23 +207,26 @@ hipError_t launch_rope(const RopeArgs& a) {
   P.sign = a.inverse ? -1.0 : 1.0;
   P.ids = a.ids;
   P.ids_stride = a.ids_stride;
-  const int tiles = (a.tokens + kRopeTokens - 1) / kRopeTokens;
   // Heads in groups of kRopeUnroll: forming a token's angles again for every four heads is
   // cheaper than a workgroup that walks through all of them (40 + 40 heads of 720p: 580 us,
   // against 628 with all heads in one group and 596 in ten of eight).
   const int groups = (heads + kRopeUnroll - 1) / kRopeUnroll;
   P.heads_per_group = (heads + groups - 1) / groups;
-  const dim3 grid(tiles, (heads + P.heads_per_group - 1) / P.heads_per_group, a.batch);
   // Outputs that the 256 MB last-level cache would not keep for the next call leave it
   // alone: 580 -> 568 us at 720p (1.5 GB). Smaller ones stay (4680 tokens of 48 heads in
   // fp32, 115 MB: 41.4 us, 44.4 past the cache).
   const int64_t bytes = (int64_t)a.batch * heads * a.tokens * kHeadDim * (a.dtype == 2 ? 4 : 2);
   const bool stream = bytes > ((int64_t)128 << 20);
   auto launch = [&](auto small, auto large) {
-    if (stream)
-      large<<<grid, kRopeThreads, 0, a.stream>>>(P);
-    else
-      small<<<grid, kRopeThreads, 0, a.stream>>>(P);
+    for (int64_t n0 = 0; n0 < a.tokens; n0 += kRopeMost) {
+      const int64_t tiles = (std::min(a.tokens - n0, kRopeMost) + kRopeTokens - 1) / kRopeTokens;
+      const dim3 grid((unsigned)tiles, (heads + P.heads_per_group - 1) / P.heads_per_group, a.batch);
+      P.n0 = (int)n0;
+      if (stream)
+        large<<<grid, kRopeThreads, 0, a.stream>>>(P);
+      else
+        small<<<grid, kRopeThreads, 0, a.stream>>>(P);
+    }
   };
   switch (a.dtype) {
     case 0: launch(rope_kernel<bf16x8, false>, rope_kernel<bf16x8, true>); break;

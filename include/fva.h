@@ -563,7 +563,9 @@ fva_status fva_attn_cache_workspace_size(const fva_qkv_desc* q_desc, const fva_c
  * Errors: FVA_ERR_INVALID_ARG (NULL or misaligned pointers, negative max_q,
  * frame or window, scale), FVA_ERR_SHAPE (batch != 1, heads not a multiple of
  * the cache's, overlapping rows), FVA_ERR_UNSUPPORTED (head_dim, page,
- * a larger pool, table_width * page >= 2^30, 2^31 rows or work items),
+ * a larger pool, table_width * page >= 2^30, 2^31 rows of Q, 2^24 work items:
+ * a stream's every started 16 or 128 query rows of a K/V head, or a part of
+ * their keys),
  * FVA_ERR_WORKSPACE.
  */
 fva_status fva_attn_cache(const void* Q, const fva_qkv_desc* q_desc, const fva_cache* cache,

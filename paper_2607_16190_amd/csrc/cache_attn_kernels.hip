@@ -1291,25 +1291,28 @@ Sizes sizes_of(bool big, int tokens, int heads, int kv_heads, int streams, int64
 // 11.3 / 23.5 / 23.0 us in small tiles, 13.2 / 13.4 / 29.8 / 32.7 in large ones; longer
 // streams, whose merge small tiles make longer, 441 / 3384 / 8192 / 12384 turns 14.9 / 25.2
 // / 34.1 / 55.8 against 19.8 / 27.6 / 29.5 / 38.1.
+constexpr int kFewTurns = 16384, kManyTurns = 4096;
 bool is_big(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys, int window, int frame) {
   const int group = heads / kv_heads;
   if ((int64_t)max_q * group <= kRows) return false;
   const int64_t keys = sizes_of(false, tokens, heads, kv_heads, streams, most_keys, window, frame).keys;
   const double turns = (double)tiles_of(tokens, group, kRows, streams) * kv_heads * (double)((keys + kKeys - 1) / kKeys);
-  return turns > (few_keys(keys) ? 16384 : 4096);
+  return turns > (few_keys(keys) ? kFewTurns : kManyTurns);
 }
 
 }  // namespace
 
 // Both queries hold for either kernel, as a window, which they are not told, may change the
-// choice.
-int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
-  int64_t most = 0;
-  for (int big = 0; big <= ((int64_t)max_q * (heads / kv_heads) > kRows ? 1 : 0); ++big) {
+// choice (but for small tiles past kFewTurns, which none makes).
+bool cache_attn_fits(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys) {
+  const bool may_be_big = (int64_t)max_q * (heads / kv_heads) > kRows;
+  for (int big = 0; big <= (may_be_big ? 1 : 0); ++big) {
     const Sizes z = sizes_of(big, tokens, heads, kv_heads, streams, most_keys, 0, 0);
-    most = std::max(most, std::max(z.items, z.tiles * (z.rows / 16)) * kv_heads + kXcds);
+    if (!big && may_be_big && z.tiles * kv_heads > kFewTurns) continue;
+    const int64_t merges = z.slots ? z.tiles * (z.rows / 16) : 0;
+    if (std::max(z.items, merges) * kv_heads + kXcds > kCacheWorkgroups) return false;
   }
-  return most;
+  return true;
 }
 
 static size_t partial_floats(const Sizes& z, int kv_heads) { return (size_t)z.partials * kv_heads * z.rows * (kHeadDim + 2); }

@@ -440,7 +440,7 @@ fva_status check_cache_attn(const fva_qkv_desc* d, int32_t kv_heads, int32_t pag
   if (table_width <= 0 || streams < 0) return FVA_ERR_SHAPE;
   if ((int64_t)table_width * page > INT32_MAX / 2) return FVA_ERR_UNSUPPORTED;
   if ((int64_t)d->tokens * d->heads > INT32_MAX) return FVA_ERR_UNSUPPORTED;
-  if (fva::cache_attn_items(d->tokens, d->heads, kv_heads, streams, max_q, (int64_t)table_width * page) > INT32_MAX)
+  if (!fva::cache_attn_fits(d->tokens, d->heads, kv_heads, streams, max_q, (int64_t)table_width * page))
     return FVA_ERR_UNSUPPORTED;
   return FVA_OK;
 }

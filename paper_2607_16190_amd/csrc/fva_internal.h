@@ -187,7 +187,10 @@ struct CacheAttnArgs {
 
 hipError_t launch_cache_plan(const PlanArgs& a);
 hipError_t launch_cache_store(StoreArgs a);
-int64_t cache_attn_items(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys);
+// Workgroups of up to 256 threads of a call: a grid of 2^32 threads and more is cut to 32 bits
+// without an error.
+constexpr int64_t kCacheWorkgroups = ((int64_t)1 << 24) - 1;
+bool cache_attn_fits(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys);
 size_t cache_attn_workspace_bytes(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys);
 hipError_t launch_cache_attn(CacheAttnArgs a);
 

@@ -553,7 +553,8 @@ fva_status fva_attn_cache_workspace_size(const fva_qkv_desc* q_desc, const fva_c
  * statistics, P rounded to bf16 for its product, bf16 output.
  *
  * kv_len, q_start: device int32 [streams], [streams + 1], q_start ascending.
- * Lengths past the table's width are cut to it. Of the block table only the
+ * Rows past Q's tokens are left out (the others of their stream keep their
+ * positions). Lengths past the table's width are cut to it. Of the block table only the
  * entries of visible keys are read; their pages must be the stream's (a value
  * outside the pool reads some page of it). max_q: the longest stream's rows,
  * an estimate that only chooses the kernel. softmax_scale <= 0 selects

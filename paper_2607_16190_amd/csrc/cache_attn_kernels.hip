@@ -69,7 +69,8 @@ __device__ __forceinline__ int divide(int n, const Divisor& d) { return (int)(((
 
 // One stream's share of the work: its rows, keys and tiles.
 struct Stream {
-  int q0, q_len;  // first token row, tokens
+  int q0, q_len;  // first token row, tokens (those past Q's rows left out)
+  int p0;         // position of the first of them
   int kv_len;
   int tiles;
   int span;       // keys that any of its tiles sees, at most
@@ -81,9 +82,11 @@ __device__ __forceinline__ Stream stream_of(const CacheAttnArgs& P, int s) {
   Stream r;
   // Lengths and starts come from device memory: clamped, so that no index leaves the
   // tensors whatever they hold.
-  r.q0 = min(max(P.q_start[s], 0), P.tokens);
-  r.q_len = min(max(P.q_start[s + 1], r.q0), P.tokens) - r.q0;
+  const int start = max(P.q_start[s], 0), end = max(P.q_start[s + 1], start);
+  r.q0 = min(start, P.tokens);
+  r.q_len = min(end, P.tokens) - r.q0;
   r.kv_len = min(max(P.kv_len[s], 0), P.width << P.page_shift);
+  r.p0 = r.kv_len - (end - start);
   r.tiles = (int)(((uint32_t)(r.q_len * P.group) + (uint32_t)P.rows - 1) >> P.row_shift);
   r.span = min(r.kv_len, P.most_keys);
   r.mean = P.ramp ? min(r.span, max(r.kv_len - (r.q_len >> 1), (r.kv_len + 1) >> 1)) : r.span;
@@ -124,7 +127,7 @@ struct Work {
   int items;     // of all, per K/V head
 };
 
-__device__ __forceinline__ Stream none() { return Stream{0, 0, 0, 0, 0, 0, 1}; }
+__device__ __forceinline__ Stream none() { return Stream{0, 0, 0, 0, 0, 0, 0, 1}; }
 
 __device__ __forceinline__ Stream stream_in(const CacheAttnArgs& P, int s, int chunk) {
   if (s >= P.streams) return none();
@@ -265,14 +268,14 @@ __device__ __forceinline__ int chunk_keys(const CacheAttnArgs& P, const Stream& 
 }
 
 __device__ __forceinline__ Stream lane_stream(const Stream& r, int l) {
-  return Stream{__builtin_amdgcn_readlane(r.q0, l),   __builtin_amdgcn_readlane(r.q_len, l), __builtin_amdgcn_readlane(r.kv_len, l),
-                __builtin_amdgcn_readlane(r.tiles, l), __builtin_amdgcn_readlane(r.span, l),  __builtin_amdgcn_readlane(r.mean, l),
-                __builtin_amdgcn_readlane(r.chunks, l)};
+  return Stream{__builtin_amdgcn_readlane(r.q0, l),     __builtin_amdgcn_readlane(r.q_len, l), __builtin_amdgcn_readlane(r.p0, l),
+                __builtin_amdgcn_readlane(r.kv_len, l), __builtin_amdgcn_readlane(r.tiles, l), __builtin_amdgcn_readlane(r.span, l),
+                __builtin_amdgcn_readlane(r.mean, l),   __builtin_amdgcn_readlane(r.chunks, l)};
 }
 
 // Keys [lo, hi) that token i of a stream sees.
 __device__ __forceinline__ void visible(const CacheAttnArgs& P, const Stream& st, int i, int& lo, int& hi) {
-  const int p = st.kv_len - st.q_len + i;
+  const int p = st.p0 + i;
   int64_t end = st.kv_len;
   if (P.frame) end = p < 0 ? 0 : ((int64_t)divide(p, P.by_frame) + 1) * P.frame;
   hi = (int)min(end, (int64_t)st.kv_len);

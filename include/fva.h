@@ -550,14 +550,18 @@ fva_status fva_attn_cache_workspace_size(const fva_qkv_desc* q_desc, const fva_c
  * cache, 1 is causal by token, H * W is causal by frame with the own frame
  * whole. O = softmax(softmax_scale * Q . K) V over them, 0 for a row that sees
  * none. The cached values enter the products exactly; fp32 accumulation and
- * statistics, P rounded to bf16 for its product, bf16 output.
+ * statistics, P rounded to bf16 for its product, bf16 output. Calls of many
+ * rows (tiles of 128) take Q as two E4M3 codes an element: exact from 2^-13 of
+ * the row's largest element on, within 2^-21 of that element below. Scores
+ * have to stay below 2^30 in magnitude.
  *
  * kv_len, q_start: device int32 [streams], [streams + 1], q_start ascending.
  * Rows past Q's tokens are left out (the others of their stream keep their
  * positions). Lengths past the table's width are cut to it. Of the block table only the
  * entries of visible keys are read; their pages must be the stream's (a value
  * outside the pool reads some page of it). max_q: the longest stream's rows,
- * an estimate that only chooses the kernel. softmax_scale <= 0 selects
+ * an estimate that, with the sizes, the table's width among them, only chooses
+ * the kernel: results may differ in their rounding. softmax_scale <= 0 selects
  * 1/sqrt(128). O: Q's strides; rows of no stream are left as they were.
  * workspace: as queried (NULL if 0), 256-byte aligned. Results do not depend
  * on the run: partial results are merged in a fixed order.

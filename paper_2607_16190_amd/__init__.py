@@ -581,7 +581,8 @@ def fva_rope(q, k, hw, dims, *, ids=None, origin=(0, 0, 0), theta: float = 10000
 
     hw: rows and columns of a frame; dims: channels turned by (t, y, x); ids: int32 [tokens] or [batch, tokens]
     token ids, or None for raster order; inverse: the gradient's direction; out: the tensor(s) written, which may be
-    the inputs. Returns q turned, or (q, k) turned.
+    the inputs. Returns q turned, or (q, k) turned. Like every call here it records nothing for autograd: the gradient
+    of q is this call with inverse=True on the gradient of its output.
     """
     if q.dtype not in _DTYPES or (k is not None and k.dtype != q.dtype):
         raise ValueError("q and k must share one of bf16, fp16 and fp32")

@@ -11,7 +11,7 @@
 // Work item = (tile, chunk of its keys), one workgroup per item and K/V head. The chunk
 // length follows from the lengths on the device (work_of), the same in every wave: as many
 // items as the chip holds workgroups, where the tiles alone are fewer (of large tiles, as
-// many as fill whole rounds of workgroups). A tile in several chunks leaves unnormalised
+// many as are estimated to end first). A tile in several chunks leaves unnormalised
 // partial results that cache_combine_kernel merges in chunk order (no atomics: the result
 // is the same on every run).
 //
@@ -1293,7 +1293,8 @@ Sizes sizes_of(bool big, int tokens, int heads, int kv_heads, int streams, int64
 // 16 rows x 64 keys: streams of up to 2048 keys 1170 / 3800 / 10240 / 12250 turns 10.5 /
 // 11.3 / 23.5 / 23.0 us in small tiles, 13.2 / 13.4 / 29.8 / 32.7 in large ones; longer
 // streams, whose merge small tiles make longer, 441 / 3384 / 8192 / 12384 turns 14.9 / 25.2
-// / 34.1 / 55.8 against 19.8 / 27.6 / 29.5 / 38.1.
+// / 34.1 / 55.8 against 19.8 / 27.6 / 29.5 / 38.1. (Keys are those that the table's width and
+// the window allow: the lengths are not known here.)
 constexpr int kFewTurns = 16384, kManyTurns = 4096;
 bool is_big(int tokens, int heads, int kv_heads, int streams, int max_q, int64_t most_keys, int window, int frame) {
   const int group = heads / kv_heads;

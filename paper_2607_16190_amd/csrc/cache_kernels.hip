@@ -334,8 +334,9 @@ void launch_store(const StoreArgs& a, dim3 grid) {
 
 hipError_t launch_cache_plan(const PlanArgs& a) {
   (void)hipGetLastError();
-  // Four rows a thread; the ring entries of a call are fewer than its token rows or are
-  // gone through by the same loop.
+  // Four rows a thread. The pages that ended streams give back go through the same grid, so that
+  // a call of few rows that ends many long streams takes longer: 64 streams of 30,000 tokens (30,016
+  // pages) 68 us in one workgroup, 6.5 in the 30 of 30,000 rows.
   const int grid = (int)std::min<int64_t>(256, std::max<int64_t>(1, ((int64_t)a.tokens + 4 * kPlanThreads - 1) / (4 * kPlanThreads)));
   cache_plan_kernel<<<grid, kPlanThreads, 0, a.stream>>>(a);
   return hipGetLastError();

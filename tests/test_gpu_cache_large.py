@@ -143,3 +143,38 @@ def test_starts_that_are_not_ascending_stay_in_bounds():
     around.fill_(5.0)
     attend(c, 1, start=[40, 80, 80, 120], out=out)
     assert bool((out[:, :, :40] == 5).all()) and bool((out[:, :, 120:] == 5).all()) and bool(out[:, :, 40:120].isfinite().all())
+
+
+def test_captured_call_on_new_lengths():
+    """A captured call of large tiles, split and whole by the lengths of the moment, against eager calls."""
+    c = upload(attn_case([9000, 4000], [300, 200], 64, 16, 8, seed=8))
+    lens, start = i32(c["lens"]), i32([0, 300, 500])
+    call = lambda: fva.fva_attn_cache(c["q"], *c["dev"], lens, start, 300, frame=1)  # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for n in ([9000, 4000], [300, 200], [9000, 0], [1200, 3999], [0, 0], [8999, 250], [9000, 4000]):
+        lens.copy_(i32(n))
+        graph.replay()
+        want = call()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), n
+
+
+def test_two_streams_at_once():
+    cases = [upload(attn_case([5000 + 300 * i], [200], 64, 16, 8, seed=i)) for i in (0, 1)]
+    want = [attend(c, 1) for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        got = []
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                got.append(attend(c, 1))
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for g, w in zip(got, want))

@@ -453,8 +453,8 @@ fva_status fva_rope(const void* Q, void* Q_out, const fva_qkv_desc* q_desc, cons
  * k_exp, v_exp int32 [pages, heads], one power-of-two scale for each page and
  * head: the value of a code is E4M3(code) * 2^e, with e = max(-100, min{e :
  * amax * 2^-e <= 448}) over the page's tokens of that head, which is at most
- * 120 (the e of infinities). Token j of stream
- * s lies in page block_table[s, j / page] at j % page; block_table is int32
+ * 120 (the e of infinities). Token j of stream s lies in page
+ * block_table[s, j / page] at j % page; block_table is int32
  * [streams, table_width]. All of it is the caller's memory. A pool has fewer
  * than 2^31 slots and 2^29 page heads (pages * heads).
  *
@@ -557,8 +557,8 @@ fva_status fva_attn_cache_workspace_size(const fva_qkv_desc* q_desc, const fva_c
  *
  * kv_len, q_start: device int32 [streams], [streams + 1], q_start ascending.
  * Rows past Q's tokens are left out (the others of their stream keep their
- * positions). Lengths past the table's width are cut to it. Of the block table only the
- * entries of visible keys are read; their pages must be the stream's (a value
+ * positions). Lengths past the table's width are cut to it. Of the block table
+ * only the entries of visible keys are read; their pages must be the stream's (a value
  * outside the pool reads some page of it). max_q: the longest stream's rows,
  * an estimate that, with the sizes, the table's width among them, only chooses
  * the kernel: results may differ in their rounding. softmax_scale <= 0 selects

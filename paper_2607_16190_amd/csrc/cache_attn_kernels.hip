@@ -16,9 +16,9 @@
 // is the same on every run).
 //
 // Codes enter the products exactly (E4M3 has four significant bits; bf16 holds them times
-// the page's power of two; V's times 2^-kValueDown of it, see there); accumulation, statistics and sums are fp32. P is rounded to
-// bf16 for its product with V, as the matrix unit takes it: at most half a step, 2^-8 of
-// each term, the same as the output's own rounding.
+// the page's power of two, V's times 2^-kValueDown of it); accumulation, statistics and sums
+// are fp32. P is rounded to bf16 for its product with V, as the matrix unit takes it: at most
+// half a step, 2^-8 of each term, the same as the output's own rounding.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -77,3 +77,27 @@ def test_huge_value_of_a_masked_key(name, page, value):
             near = np.abs(y - O) <= tol
         past = np.isinf(y) & (np.sign(y) == np.sign(O)) & (np.abs(O) + tol > BF16_MAX)
         assert (near | past).all(), i
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), 3.38e38, float("nan")])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("name", CASES)
+def test_huge_masked_key(name, page, value):
+    """The same of K, and of a NaN, which is stored as some finite value, in both."""
+    n, m, H, KH, frame, window, token, _ = CASES[name]
+    _, v8, _, ve, table, (at, off) = stored(n, page, KH, token, value, n + page)
+    _, k8, _, ke, other, _ = stored(n, page, KH, token, value, n + page + 1)
+    # K is the V of another cache, its pages put where this one's are
+    order = np.arange(len(k8))
+    order[table] = other
+    k8, ke = (t[torch.from_numpy(order).to(DEV)] for t in (k8, ke))
+    q = torch.randn((1, m, H, 128), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV).transpose(1, 2)
+    call = lambda k, v: fva.fva_attn_cache(q, k, v, ke, ve, i32(table[None]), i32([n]), i32([0, m]), m, frame=frame, window=window)  # noqa: E731
+    got = call(k8, v8)
+    plain = [t.clone() for t in (k8, v8)]
+    for t in plain:
+        t[at, :, off] = 0
+    want = call(*plain)
+    blind = torch.tensor([not lo <= token < hi for lo, hi in (visible_keys(n, m, i, frame, window) for i in range(m))])
+    assert blind.any() and want.isfinite().all()
+    assert torch.equal(got[:, :, blind], want[:, :, blind])
